@@ -1,4 +1,5 @@
-"""ctypes binding of libpreserve_mi355x.so: the same entry points as include/preserve.h and include/preserve_aux.h.
+"""ctypes binding of libpreserve_mi355x.so: the same entry points as include/preserve.h, include/preserve_aux.h and
+include/preserve_ops.h.
 
 Argument marshalling only -- every step of the decode path runs inside the library's HIP kernels.
 There is no fallback: if the built library is missing, loading raises.  Device buffers are torch
@@ -23,6 +24,12 @@ PSV_W_ROW_MAJOR, PSV_W_TILED = 0, 1
 WEIGHT_LAYOUTS = {"row": PSV_W_ROW_MAJOR, "tiled": PSV_W_TILED}
 PSV_KV_UNIT_BYTES_BF16, PSV_KV_UNIT_BYTES_INT8 = 4096, 2112
 PSV_STATIC_SCRATCH_BYTES = 16 << 20
+PSV_F32, PSV_BF16, PSV_F16 = 0, 1, 2
+PSV_ROPE_MAX_DIMS = 256
+ROPE_PAIRINGS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "turns": 2, "channel": 3}
+PSV_SLOTS_MAX_BATCH = 4096
+PSV_LOGPROBS_MAX_TOP, PSV_LOGPROBS_MAX_GIVEN, PSV_LOGPROBS_MAX_RECORDS = 32, 32, 256
 PSV_DBG_H1, PSV_DBG_QKV, PSV_DBG_ATTN, PSV_DBG_Y, PSV_DBG_H2, PSV_DBG_M = range(6)
 
 EXPORTS = [
@@ -33,6 +40,12 @@ EXPORTS = [
     "psv_set_profile_op",
     "psv_get_profile", "psv_prefetch_region", "psv_spin", "psv_copy_bytes", "psv_debug_read",
     "psv_debug_force_wait_timeout", "psv_decode_step_static", "psv_set_fused_kernels", "psv_debug_last_step_path", "psv_debug_last_step_prelaunches", "psv_debug_last_step_read_once", "psv_tile_weights",
+]
+
+# the operators around the decode step (include/preserve_ops.h)
+OPERATOR_EXPORTS = [
+    "psv_rope_plan", "psv_set_rope", "psv_rotate", "psv_cache_slots", "psv_cache_append", "psv_cache_gather", "psv_logprobs_records",
+    "psv_logprobs_bytes", "psv_logprobs_part", "psv_logprobs_join", "psv_logprobs",
 ]
 
 
@@ -71,6 +84,59 @@ class psv_stats(C.Structure):
                 ("planned_prefetch_bytes", C.c_uint64), ("workspace_bytes", C.c_uint64),
                 ("kernels_per_layer", C.c_uint32), ("prefetch_launches", C.c_uint32),
                 ("steps", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class psv_rope_desc(C.Structure):
+    _fields_ = [("dims", C.c_uint32), ("pairing", C.c_uint32), ("scaling", C.c_uint32), ("reserved", C.c_uint32),
+                ("magnitude", C.c_double),
+                ("theta", C.c_double), ("factor", C.c_double), ("low_turns", C.c_double), ("high_turns", C.c_double),
+                ("trained_context", C.c_double)]
+
+
+class psv_rope(C.Structure):
+    _fields_ = [("dims", C.c_uint32), ("pairing", C.c_uint32), ("magnitude", C.c_double),
+                ("freq", C.c_double * (PSV_ROPE_MAX_DIMS // 2))]
+
+
+class psv_rotate_args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("positions", C.c_void_p), ("rows", C.c_uint32), ("heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("dtype", C.c_uint32), ("transpose", C.c_uint32), ("reserved", C.c_uint32),
+                ("x_row", C.c_int64), ("x_head", C.c_int64), ("y_row", C.c_int64), ("y_head", C.c_int64)]
+
+
+class psv_slots_args(C.Structure):
+    _fields_ = [("lens", C.c_void_p), ("new_lens", C.c_void_p), ("block_table", C.c_void_p), ("free_blocks", C.c_void_p),
+                ("free_range", C.c_void_p), ("free_capacity", C.c_uint32), ("batch", C.c_uint32), ("max_blocks", C.c_uint32),
+                ("num_pool_blocks", C.c_uint32), ("rows", C.c_uint32), ("reserved", C.c_uint32), ("seq_lens", C.c_void_p),
+                ("row_starts", C.c_void_p), ("slots", C.c_void_p), ("positions", C.c_void_p), ("requests", C.c_void_p),
+                ("free_range_out", C.c_void_p), ("refused", C.c_void_p)]
+
+
+class psv_cache(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("n_kv_heads", C.c_uint32), ("kv_format", C.c_uint32),
+                ("kv_layout", C.c_uint32), ("num_pool_blocks", C.c_uint32)]
+
+
+class psv_append_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p), ("positions", C.c_void_p),
+                ("slots", C.c_void_p), ("rows", C.c_uint32), ("n_q_heads", C.c_uint32), ("dtype", C.c_uint32),
+                ("reserved", C.c_uint32), ("q_row", C.c_int64), ("k_row", C.c_int64), ("v_row", C.c_int64),
+                ("q_out_row", C.c_int64)]
+
+
+class psv_gather_args(C.Structure):
+    _fields_ = [("slots", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("rows", C.c_uint32), ("dtype", C.c_uint32),
+                ("k_row", C.c_int64), ("v_row", C.c_int64)]
+
+
+class psv_logprobs_args(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("tokens", C.c_void_p), ("rows", C.c_uint32), ("columns", C.c_uint32),
+                ("first_token", C.c_uint32), ("vocab", C.c_uint32), ("dtype", C.c_uint32), ("given", C.c_uint32),
+                ("top", C.c_uint32), ("scale", C.c_float), ("records", C.c_uint32), ("reserved", C.c_uint32), ("row", C.c_int64)]
+
+
+class psv_logprobs_out(C.Structure):
+    _fields_ = [("logprobs", C.c_void_p), ("entropy", C.c_void_p), ("top_logprobs", C.c_void_p), ("top_ids", C.c_void_p)]
 
 
 class PsvError(RuntimeError):
@@ -126,6 +192,17 @@ def lib():
             "psv_set_fused_kernels": (C.c_int32, [vp, u32]),
             "psv_decode_step_static": (C.c_int32, [C.POINTER(psv_model_desc), C.POINTER(psv_layer_weights),
                                                    C.POINTER(psv_kv_desc), vp, vp, u32, u32, u32, vp]),
+            "psv_rope_plan": (C.c_int32, [C.POINTER(psv_rope_desc), C.POINTER(psv_rope)]),
+            "psv_set_rope": (C.c_int32, [vp, C.POINTER(psv_rope)]),
+            "psv_rotate": (C.c_int32, [C.POINTER(psv_rotate_args), C.POINTER(psv_rope), vp]),
+            "psv_cache_slots": (C.c_int32, [C.POINTER(psv_slots_args), vp]),
+            "psv_cache_append": (C.c_int32, [C.POINTER(psv_append_args), C.POINTER(psv_cache), C.POINTER(psv_rope), vp]),
+            "psv_cache_gather": (C.c_int32, [C.POINTER(psv_gather_args), C.POINTER(psv_cache), vp]),
+            "psv_logprobs_records": (u32, [u32, u32]),
+            "psv_logprobs_bytes": (sz, [u32, u32, u32, u32]),
+            "psv_logprobs_part": (C.c_int32, [C.POINTER(psv_logprobs_args), vp, vp]),
+            "psv_logprobs_join": (C.c_int32, [C.POINTER(psv_logprobs_args), vp, u32, C.POINTER(psv_logprobs_out), vp]),
+            "psv_logprobs": (C.c_int32, [C.POINTER(psv_logprobs_args), C.POINTER(psv_logprobs_out), vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -347,3 +424,163 @@ def psv_debug_last_step_read_once(ctx):
 
 def psv_debug_force_wait_timeout(ctx, on):
     _check(lib().psv_debug_force_wait_timeout(ctx, 1 if on else 0), "psv_debug_force_wait_timeout")
+
+
+# ---- operators around the decode step (include/preserve_ops.h) -----------------------------------------------------------
+
+
+def _rows(name, t):
+    """(dtype code, row stride) of rows [rows, heads, channels] whose heads and channels are adjacent."""
+    if t.dim() != 3 or t.shape[2] != 128 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != 128):
+        raise ValueError("%s: rows of [heads][128] adjacent elements are wanted, got shape %s, strides %s" % (name, tuple(t.shape), t.stride()))
+    return _dtype(name, t), t.stride(0)
+
+
+def _dtype(name, t):
+    code = {"torch.float32": PSV_F32, "torch.bfloat16": PSV_BF16, "torch.float16": PSV_F16}.get(str(t.dtype))
+    if code is None:
+        raise ValueError("%s: float32, bfloat16 or float16 is wanted, got %s" % (name, t.dtype))
+    return code
+
+
+def _want(name, t, dtype, *shape):
+    """A contiguous tensor of a type and shape; None where an axis may have any length."""
+    if str(t.dtype) != "torch." + dtype or not t.is_contiguous() or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError("%s: contiguous %s %s is wanted, got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
+    return t.data_ptr()
+
+
+def psv_rope_plan(dims=128, pairing="half", theta=500000.0, scaling="plain", factor=1.0, low_turns=1.0, high_turns=4.0,
+                  trained_context=8192.0, magnitude=1.0):
+    """Frequencies for psv_rotate, psv_cache_append and psv_set_rope; pairing and scaling: keys of ROPE_PAIRINGS and ROPE_SCALINGS."""
+    desc = psv_rope_desc(dims, ROPE_PAIRINGS[pairing], ROPE_SCALINGS[scaling], 0, magnitude, theta, factor, low_turns, high_turns, trained_context)
+    out = psv_rope()
+    _check(lib().psv_rope_plan(C.byref(desc), C.byref(out)), "psv_rope_plan")
+    return out
+
+
+def psv_set_rope(ctx, rope):
+    _check(lib().psv_set_rope(ctx, None if rope is None else C.byref(rope)), "psv_set_rope")
+
+
+def psv_rotate(x, y, positions, rope, stream, transpose=False):
+    """x, y: [rows, heads, channels] of one type, any strides with adjacent channels; positions: int32 [rows]."""
+    rows, heads, dim = x.shape
+    if y.shape != x.shape or y.dtype != x.dtype or (dim > 1 and (x.stride(2) != 1 or y.stride(2) != 1)):
+        raise ValueError("psv_rotate: x and y of one shape and type with adjacent channels are wanted")
+    a = psv_rotate_args(x.data_ptr(), y.data_ptr(), _want("positions", positions, "int32", rows), rows, heads, dim, _dtype("x", x),
+                        1 if transpose else 0, 0, x.stride(0), x.stride(1), y.stride(0), y.stride(1))
+    _check(lib().psv_rotate(C.byref(a), C.byref(rope), _stream(stream)), "psv_rotate")
+
+
+def psv_cache_slots(lens, new_lens, block_table, free_blocks, free_range, num_pool_blocks, seq_lens, row_starts, slots, positions,
+                    requests, free_range_out, refused, stream, max_blocks=None):
+    """Tensors as in psv_slots_args (int32; slots int64); block_table, free_blocks, free_range, free_range_out None and max_blocks given
+    for a contiguous cache."""
+    n, rows = lens.shape[0], slots.shape[0]
+    table = block_table is not None
+    mb = block_table.shape[1] if table else int(max_blocks)
+    a = psv_slots_args(_want("lens", lens, "int32", n), _want("new_lens", new_lens, "int32", n),
+                       _want("block_table", block_table, "int32", n, None) if table else None,
+                       _want("free_blocks", free_blocks, "int32", None) if table else None,
+                       _want("free_range", free_range, "int32", 2) if table else None, free_blocks.shape[0] if table else 0, n, mb,
+                       num_pool_blocks, rows, 0, _want("seq_lens", seq_lens, "int32", n), _want("row_starts", row_starts, "int32", n + 1),
+                       _want("slots", slots, "int64", rows), _want("positions", positions, "int32", rows),
+                       _want("requests", requests, "int32", rows), _want("free_range_out", free_range_out, "int32", 2) if table else None,
+                       _want("refused", refused, "int32", 1))
+    _check(lib().psv_cache_slots(C.byref(a), _stream(stream)), "psv_cache_slots")
+
+
+def kv_cache(k_pool, v_pool, n_kv_heads, kv_format, kv_layout, num_pool_blocks):
+    """One layer's pools; kv_format, kv_layout: keys of FORMATS and KV_LAYOUTS."""
+    return psv_cache(_dev_ptr(k_pool), _dev_ptr(v_pool), n_kv_heads, FORMATS[kv_format], KV_LAYOUTS[kv_layout], num_pool_blocks)
+
+
+def psv_cache_append(q, k, v, q_out, positions, slots, cache, rope, stream):
+    """q, q_out [rows, q heads, 128], or None; k, v [rows, kv heads, 128]; positions int32 [rows] (None without rope); slots int64 [rows]."""
+    rows = k.shape[0]
+    dt, k_row = _rows("k", k)
+    dv, v_row = _rows("v", v)
+    if dv != dt or v.shape != k.shape or k.shape[1] != cache.n_kv_heads:
+        raise ValueError("psv_cache_append: k and v of one type with the cache's %d heads are wanted" % cache.n_kv_heads)
+    nq = q_row = q_out_row = 0
+    if q is not None:
+        (dq, q_row), (do, q_out_row), nq = _rows("q", q), _rows("q_out", q_out), q.shape[1]
+        if dq != dt or do != dt or q_out.shape != q.shape or q.shape[0] != rows:
+            raise ValueError("psv_cache_append: q and q_out of k's type and rows are wanted")
+    a = psv_append_args(_dev_ptr(q), k.data_ptr(), v.data_ptr(), None if q is None else q_out.data_ptr(),
+                        None if positions is None else _want("positions", positions, "int32", rows), _want("slots", slots, "int64", rows),
+                        rows, nq, dt, 0, q_row, k_row, v_row, q_out_row)
+    _check(lib().psv_cache_append(C.byref(a), C.byref(cache), None if rope is None else C.byref(rope), _stream(stream)), "psv_cache_append")
+
+
+def psv_cache_gather(slots, k, v, cache, stream):
+    """slots int64 [rows]; k, v [rows, kv heads, 128] of one type."""
+    rows = slots.shape[0]
+    dt, k_row = _rows("k", k)
+    dv, v_row = _rows("v", v)
+    if dv != dt or v.shape != k.shape or k.shape[0] != rows or k.shape[1] != cache.n_kv_heads:
+        raise ValueError("psv_cache_gather: k and v of one type with %d rows of the cache's %d heads are wanted" % (rows, cache.n_kv_heads))
+    a = psv_gather_args(_want("slots", slots, "int64", rows), k.data_ptr(), v.data_ptr(), rows, dt, k_row, v_row)
+    _check(lib().psv_cache_gather(C.byref(a), C.byref(cache), _stream(stream)), "psv_cache_gather")
+
+
+def psv_logprobs_records(rows, columns):
+    return int(lib().psv_logprobs_records(rows, columns))
+
+
+def psv_logprobs_bytes(rows, records, given, top):
+    return int(lib().psv_logprobs_bytes(rows, records, given, top))
+
+
+def _logprobs_args(rows, logits, tokens, scale, top, first_token, vocab, records):
+    given = 0 if tokens is None else tokens.shape[1]
+    columns, row, dt = 0, 0, PSV_F32
+    if logits is not None:
+        if logits.dim() != 2 or logits.shape[0] != rows or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise ValueError("logits: [rows, columns] with adjacent columns are wanted")
+        columns, row, dt = logits.shape[1], max(logits.stride(0), logits.shape[1]) if rows == 1 else logits.stride(0), _dtype("logits", logits)
+    return psv_logprobs_args(_dev_ptr(logits), None if given == 0 else _want("tokens", tokens, "int32", rows, given), rows, columns, first_token,
+                             columns if vocab is None else vocab, dt, given, top, scale, records, 0, row)
+
+
+def _logprobs_out(rows, given, logprobs, entropy, top_logprobs, top_ids):
+    top = 0 if top_ids is None else top_ids.shape[1]
+    return psv_logprobs_out(None if logprobs is None else _want("logprobs", logprobs, "float32", rows, given),
+                            None if entropy is None else _want("entropy", entropy, "float32", rows),
+                            None if top == 0 else _want("top_logprobs", top_logprobs, "float32", rows, top),
+                            None if top == 0 else _want("top_ids", top_ids, "int32", rows, top)), top
+
+
+def _bytes_of(t):
+    return t.numel() * t.element_size()
+
+
+def psv_logprobs_part(logits, tokens, scale, top, records_out, stream, first_token=0, vocab=None, records=0):
+    """logits [rows, columns]: a shard's columns of the vocabulary; tokens int32 [rows, given] or None; records_out: a tensor of at least
+    psv_logprobs_bytes bytes."""
+    rows = logits.shape[0]
+    a = _logprobs_args(rows, logits, tokens, scale, top, first_token, vocab, records)
+    if rows and _bytes_of(records_out) < psv_logprobs_bytes(rows, records or psv_logprobs_records(rows, a.columns), a.given, top):
+        raise ValueError("psv_logprobs_part: the records do not fit their tensor")
+    _check(lib().psv_logprobs_part(C.byref(a), _dev_ptr(records_out), _stream(stream)), "psv_logprobs_part")
+
+
+def psv_logprobs_join(rows, tokens, scale, vocab, records, shards, logprobs, entropy, top_logprobs, top_ids, records_in, stream, top=None):
+    """records_in: the shards' records of psv_logprobs_part behind one another; top: of the records (top_ids's width by default)."""
+    out, n = _logprobs_out(rows, 0 if tokens is None else tokens.shape[1], logprobs, entropy, top_logprobs, top_ids)
+    if top is not None and n not in (0, top):
+        raise ValueError("psv_logprobs_join: top_ids is [rows, top]")
+    a = _logprobs_args(rows, None, tokens, scale, n if top is None else top, 0, vocab, records)
+    if rows and _bytes_of(records_in) < shards * psv_logprobs_bytes(rows, records, a.given, a.top):
+        raise ValueError("psv_logprobs_join: %d shards of %d records a row are wanted" % (shards, records))
+    _check(lib().psv_logprobs_join(C.byref(a), _dev_ptr(records_in), shards, C.byref(out), _stream(stream)), "psv_logprobs_join")
+
+
+def psv_logprobs(logits, tokens, scale, logprobs, entropy, top_logprobs, top_ids, workspace, stream):
+    """logits [rows, vocabulary]; tokens int32 [rows, given] or None; the outputs, any of them None; workspace: a tensor of at least
+    psv_logprobs_bytes bytes."""
+    rows = logits.shape[0]
+    out, top = _logprobs_out(rows, 0 if tokens is None else tokens.shape[1], logprobs, entropy, top_logprobs, top_ids)
+    a = _logprobs_args(rows, logits, tokens, scale, top, 0, None, 0)
+    _check(lib().psv_logprobs(C.byref(a), C.byref(out), _dev_ptr(workspace), _bytes_of(workspace), _stream(stream)), "psv_logprobs")

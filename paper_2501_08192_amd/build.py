@@ -7,9 +7,12 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpreserve_mi355x.so")
-SOURCES = ["gemv.hip", "gemm_sk.hip", "attention.hip", "window.hip", "segment.hip", "step.hip", "static_step.hip", "executor.cpp", "api.cpp", "planner.cpp"]
+SOURCES = ["gemv.hip", "gemm_sk.hip", "attention.hip", "window.hip", "segment.hip", "step.hip", "static_step.hip", "rotary.hip", "cache_rows.hip", "slots.hip", "logprobs.hip",
+           "executor.cpp", "api.cpp", "operators.cpp", "planner.cpp"]
 HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "device.h"), os.path.join(CSRC, "context.h"), os.path.join(CSRC, "tagged.h"), os.path.join(CSRC, "prefetch.h"),
-           os.path.join(HERE, "..", "include", "preserve.h"), os.path.join(HERE, "..", "include", "preserve_aux.h")]
+           os.path.join(CSRC, "operators.h"), os.path.join(CSRC, "rows.h"),
+           os.path.join(HERE, "..", "include", "preserve.h"), os.path.join(HERE, "..", "include", "preserve_aux.h"),
+           os.path.join(HERE, "..", "include", "preserve_ops.h")]
 
 # Packed-FP32 VALU instructions are switched off for all device code.
 HIP_FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall", "-Wno-unused-result",

@@ -70,7 +70,7 @@ __device__ __forceinline__ void make_attn_plan(const int32_t *seq_lens, int max_
 // fp32 range reduction.  The position is the same for every layer, so this runs once per step -- as does the plan of the
 // attention's work, by one more workgroup (blockIdx.x == batch).
 __global__ __launch_bounds__(64) void k_rope_table(const int32_t *__restrict__ seq_lens, const double *__restrict__ inv_freq,
-                                                   int max_tokens, int batch, float2 *__restrict__ table, AttnPlan plan)
+                                                   double magnitude, int max_tokens, int batch, float2 *__restrict__ table, AttnPlan plan)
 {
     const int b = blockIdx.x, i = threadIdx.x;
     if (b == batch) {
@@ -83,16 +83,29 @@ __global__ __launch_bounds__(64) void k_rope_table(const int32_t *__restrict__ s
     if (inv_freq) {
         double sd, cd;
         sincos((double)(T - 1) * inv_freq[i], &sd, &cd);
-        cs = make_float2((float)cd, (float)sd);
+        cs = make_float2((float)(cd * magnitude), (float)(sd * magnitude));
     }
     table[b * 64 + i] = cs;
 }
 
-hipError_t launch_rope_table(const int32_t *seq_lens, const double *inv_freq, int max_tokens, int batch, float2 *table,
+hipError_t launch_rope_table(const int32_t *seq_lens, const double *inv_freq, double magnitude, int max_tokens, int batch, float2 *table,
                              const AttnPlan *plan, hipStream_t s)
 {
     if (plan && (batch > 64 || plan->slots < batch)) return hipErrorInvalidValue;
-    PSV_LAUNCH(k_rope_table, dim3(batch + (plan ? 1 : 0)), dim3(64), 0, s, seq_lens, inv_freq, max_tokens, batch, table, plan ? *plan : AttnPlan{});
+    PSV_LAUNCH(k_rope_table, dim3(batch + (plan ? 1 : 0)), dim3(64), 0, s, seq_lens, inv_freq, magnitude, max_tokens, batch, table, plan ? *plan : AttnPlan{});
+    return hipGetLastError();
+}
+
+struct FreqTable {
+    double f[64];
+};
+__global__ __launch_bounds__(64) void k_store_freq(FreqTable t, double *dst) { dst[threadIdx.x] = t.f[threadIdx.x]; }
+
+hipError_t launch_store_freq(const double *freq, double *dst, hipStream_t s)
+{
+    FreqTable t;
+    for (int i = 0; i < 64; ++i) t.f[i] = freq[i];
+    PSV_LAUNCH(k_store_freq, dim3(1), dim3(64), 0, s, t, dst);
     return hipGetLastError();
 }
 

@@ -393,13 +393,13 @@ static psv_status enqueue_whole_step(psv_ctx *c, const float *x_in, float *x_out
     }
     const KvView kv = kv_view(c, lb, 1);
     float2 *rope = c->at<float2>(c->ws.rope);
-    const double *inv_freq = d.rope_theta > 0.f ? c->at<double>(c->ws.inv_freq) : nullptr;
+    const double *inv_freq = d.rope_theta > 0.f || c->rope_set ? c->at<double>(c->ws.inv_freq) : nullptr;
     c->last_prefetch_launches = 0;
     c->last_step_prelaunches = 0;
     c->step_launches = 0;
     c->step_layers = le - lb;
     ST_TRY(prof_tag(c, -2));
-    HIP_TRY(launch_rope_table(c->kv.seq_lens, inv_freq, kv.max_tokens, 1, rope, nullptr, s));
+    HIP_TRY(launch_rope_table(c->kv.seq_lens, inv_freq, c->rope_magnitude, kv.max_tokens, 1, rope, nullptr, s));
     StepLaunch p{};
     p.layer_table = c->wsp + c->ws.step_tbl;
     p.lb = (int)lb; p.le = (int)le;
@@ -459,7 +459,7 @@ psv_status enqueue_step(psv_ctx *c, const float *x_in, float *x_out, uint32_t ba
     uint16_t *attnb = c->at<uint16_t>(c->ws.attn_bf16), *mb = c->at<uint16_t>(c->ws.m_bf16);
     float *pml = c->at<float>(c->ws.part_ml), *po = c->at<float>(c->ws.part_o);
     float2 *rope = c->at<float2>(c->ws.rope);
-    const double *inv_freq = d.rope_theta > 0.f ? c->at<double>(c->ws.inv_freq) : nullptr;
+    const double *inv_freq = d.rope_theta > 0.f || c->rope_set ? c->at<double>(c->ws.inv_freq) : nullptr;
     Lanes ln{c->main, c->side};
     hipStream_t &s = ln.cur;          // the stream the operator chain is on (changes at a pre-launching window)
     GemvWait wait{};
@@ -559,7 +559,7 @@ psv_status enqueue_step(psv_ctx *c, const float *x_in, float *x_out, uint32_t ba
     c->last_step_planned = plan != nullptr;
 
     ST_TRY(prof_tag(c, -2));
-    HIP_TRY(launch_rope_table(c->kv.seq_lens, inv_freq, kv_view(c, lb, batch).max_tokens, B, rope, made, s));
+    HIP_TRY(launch_rope_table(c->kv.seq_lens, inv_freq, c->rope_magnitude, kv_view(c, lb, batch).max_tokens, B, rope, made, s));
     const float *res = x_in, *delta = nullptr;   // residual stream entering the layer = res + delta
     int delta_splits = 1;                        // delta may be a stack of split-K partials
     for (uint32_t l = lb; l < le; ++l) {

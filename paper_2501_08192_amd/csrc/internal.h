@@ -209,9 +209,12 @@ hipError_t launch_resid_sum(const float *res, const float *delta, int delta_spli
 // Gate | up: out = silu(gate) * up of the summed splits, width N/2, also as the next projection's operand in out_bf16.
 hipError_t launch_sk_reduce(const float *part, int splits, int batch, int N, float *out, uint16_t *out_bf16, bool digits, hipStream_t s);
 
-// cos/sin of the rotary angles at position seq_len-1: table [batch][64] (inv_freq null => identity); optionally the step's plan.
-hipError_t launch_rope_table(const int32_t *seq_lens, const double *inv_freq, int max_tokens, int batch,
+// cos/sin of the rotary angles at position seq_len-1, times magnitude: table [batch][64] (inv_freq null => identity); optionally
+// the step's plan.
+hipError_t launch_rope_table(const int32_t *seq_lens, const double *inv_freq, double magnitude, int max_tokens, int batch,
                              float2 *table, const AttnPlan *plan, hipStream_t s);
+// The 64 rotary frequencies, handed over as a kernel argument: no host-to-device copy.
+hipError_t launch_store_freq(const double *freq, double *dst, hipStream_t s);
 
 // Decode attention: RoPE of q, KV append and split-K partials (max, sum, weighted V) per workgroup ...
 hipError_t launch_attn(const float *qkv, const float2 *rope, KvView kv, int batch, int nq, int nkv, AttnSplit sp,

@@ -18,12 +18,6 @@ namespace {
 constexpr int kMaxDevices = 64;
 void *g_scratch_ptr[kMaxDevices];   // device address of `scratch` on each device (null: not looked up yet)
 
-// The 64 rotary frequencies arrive as a kernel argument and are stored by the kernel: no host-to-device copy.
-struct FreqTable {
-    double f[64];
-};
-__global__ __launch_bounds__(64) void k_store_freq(FreqTable t, double *dst) { dst[threadIdx.x] = t.f[threadIdx.x]; }
-
 }  // namespace
 
 extern "C" psv_status psv_decode_step_static(const psv_model_desc *desc, const psv_layer_weights *layers,
@@ -79,10 +73,9 @@ extern "C" psv_status psv_decode_step_static(const psv_model_desc *desc, const p
         ST_TRY(psv_set_kv(&c, &k2));
     }
     if (desc->rope_theta > 0.f) {
-        FreqTable t;
-        for (int i = 0; i < 64; ++i) t.f[i] = pow((double)desc->rope_theta, -2.0 * (double)i / 128.0);
-        hipLaunchKernelGGL(k_store_freq, dim3(1), dim3(64), 0, c.main, t, c.at<double>(ws.inv_freq));
-        HIP_TRY(hipGetLastError());
+        double f[64];
+        for (int i = 0; i < 64; ++i) f[i] = pow((double)desc->rope_theta, -2.0 * (double)i / 128.0);
+        HIP_TRY(launch_store_freq(f, c.at<double>(ws.inv_freq), c.main));
     }
     // Nothing in the workspace has to start at zero for a step without windows: every buffer is written by the step
     // before it is read (the flag words of the window fork are not used here), so the previous call's contents --
