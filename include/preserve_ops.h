@@ -193,7 +193,7 @@ typedef struct {
     uint32_t dtype;
     uint32_t given;               /* tokens a row, 0 .. PSV_LOGPROBS_MAX_GIVEN */
     uint32_t top;                 /* alternatives a row, 0 .. PSV_LOGPROBS_MAX_TOP */
-    float    scale;               /* > 0, at most 2^32 */
+    float    scale;               /* 2^-32 .. 2^32 */
     uint32_t records;             /* psv_logprobs_records of this shard or of one with more columns; 0: of this one */
     uint32_t reserved;
     int64_t  row;                 /* stride in elements, >= 0 (rows start at any element) */

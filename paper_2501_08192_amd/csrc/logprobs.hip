@@ -15,80 +15,104 @@
 
 namespace psv {
 
-constexpr int kWaves = kLogprobThreads / 64;
+constexpr int kThreads = kLogprobThreads, kWaves = kThreads / 64;
 constexpr uint32_t kList = PSV_LOGPROBS_MAX_TOP * 64;
 
-// Order of floats as unsigned integers (-0 counts as 0; no NaN)
+// Order of floats as unsigned integers (-0 counts as 0, every NaN is above infinity)
 __device__ __forceinline__ uint32_t order_of(float x)
 {
     const uint32_t b = __float_as_uint(x + 0.f);
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+    return x != x ? ~0u : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float of_order(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
-constexpr uint32_t kOrderNone = 0x007fffffu;      // of -infinity
+constexpr uint32_t kOrderNone = 0x007fffffu, kOrderInf = 0xff800000u;      // of -infinity and infinity
+constexpr float kLowest = -3.402823466e38f;
 
-// The k-th largest of the workgroup's kLogprobThreads values (k <= threads), or a lower value that exactly k of them reach: bit by bit
-// from the top, counted by the lanes of one wave.
-__device__ __forceinline__ uint32_t kth_largest(uint32_t v, uint32_t k, uint32_t *tmp)
+__device__ __forceinline__ float nan32() { return __uint_as_float(0x7fc00000u); }
+
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
 {
-    tmp[threadIdx.x] = v;
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        uint32_t w[kWaves], t = 0;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) w[i] = tmp[i * 64 + threadIdx.x];
-        for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
-            uint32_t n = 0;
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i) n += __popcll(__ballot(w[i] >= (t | bit)));
-            if (n >= k) t |= bit;
-            if (n == k) break;
-        }
-        if (threadIdx.x == 0) tmp[kLogprobThreads] = t;
-    }
-    __syncthreads();
-    return tmp[kLogprobThreads];
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));
+    const uint32_t a = max((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16));
+    return max(a, max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48)));
 }
 
-// Ranks of the n listed (order, id) among themselves; the first `top` go to values and ids, what is missing is filled up.
-__device__ __forceinline__ void write_ranked(const uint2 *list, uint32_t n, uint32_t top, float *values, int32_t *ids)
+// The k-th largest of the workgroup's values (k <= threads), or a lower one that at most `enough` of them reach: bit by bit, from the first
+// in which the largest and the smallest differ down to bit LOW (below it an order has zeros, or ones where the value is negative).  A wave has
+// all of them, one of each wave a lane, and counts for itself.  Bound by the way from the comparisons to the scalar unit and back, some
+// 0.06 us a bit, so that it stops early; two bits a step took as long.
+template <int LOW, int W>
+__device__ __forceinline__ uint32_t kth_largest(const uint32_t (&w)[W], uint32_t k, uint32_t enough)
 {
-    for (uint32_t i = threadIdx.x; i < n; i += kLogprobThreads) {
-        const uint2 me = list[i];
+    uint32_t most = w[0], least = ~w[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) {
+        most = max(most, w[i]);
+        least = max(least, ~w[i]);
+    }
+    most = wave_max_u32(most);
+    least = ~wave_max_u32(least);
+    if (k == 1 || most == least) return most;
+    uint32_t bit = 0x80000000u >> __builtin_clz(most ^ least), t = least & ~(2 * bit - 1);
+    for (; bit >= 1u << LOW; bit >>= 1) {
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) n += __popcll(__ballot(w[i] >= (t | bit)));
+        if (n >= k) {
+            t |= bit;
+            if (n <= enough) break;
+        }
+    }
+    return t & 0x80000000u ? t : t | ((1u << LOW) - 1);
+}
+// How many lanes may reach the bound: as many as the list has room for, but not so many that ranking them takes longer than the bits would.
+__host__ __device__ constexpr uint32_t enough_lanes(uint32_t k, uint32_t more, uint32_t room) { return k + more < room ? k + more : room; }
+
+// Places for a lane's `n` entries in the list.  The address looks like the lane's own, or the compiler would make one addition of the wave's, by a
+// loop over its lanes: longer than what the additions take in LDS.
+__device__ __forceinline__ uint32_t list_places(uint32_t *count, uint32_t n)
+{
+    uint32_t own = 0;
+    asm volatile("" : "+v"(own));
+    return atomicAdd(count + own, n);
+}
+
+// Ranks of the n listed among themselves, an entry a lane; put(rank, entry) for the first `top`.  The others come to a wave by lane reads: an entry
+// read from LDS instead costs its latency (joining 61 rows of 160 entries for 20 of them: 5.6 us against 7.5).
+template <int THREADS, class Put>
+__device__ __forceinline__ void rank_list(const uint64_t *list, uint32_t n, uint32_t top, Put put)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    for (uint32_t i = threadIdx.x - lane; i < n; i += THREADS) {
+        const uint64_t me = list[min(i + lane, n - 1)];
         uint32_t rank = 0;
-        for (uint32_t j = 0; j < n; ++j) {
-            const uint2 o = list[j];
-            rank += o.x > me.x || (o.x == me.x && o.y < me.y);
+        for (uint32_t j0 = 0; j0 < n; j0 += 64) {
+            const uint64_t o = list[min(j0 + lane, n - 1)];
+            const uint32_t m = min(n - j0, 64u);
+            for (uint32_t j = 0; j < m; ++j) {
+                const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(o >> 32), (int)j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)o, (int)j);
+                rank += other > me;
+            }
         }
-        if (rank < top) {
-            values[rank] = of_order(me.x);
-            ids[rank] = (int32_t)me.y;
-        }
-    }
-    for (uint32_t i = n + threadIdx.x; i < top; i += kLogprobThreads) {
-        values[i] = -INFINITY;
-        ids[i] = -1;
+        if (i + lane < n && rank < top) put(rank, me);
     }
 }
+// An entry: the order of a logit, and its id so that the lower one counts as the larger.
+__device__ __forceinline__ uint64_t list_entry(uint32_t order, uint32_t id) { return (uint64_t)order << 32 | (uint32_t)~id; }
+__device__ __forceinline__ float entry_value(uint64_t v) { return of_order((uint32_t)(v >> 32)); }
+__device__ __forceinline__ uint32_t entry_id(uint64_t v) { return ~(uint32_t)v; }
 
-__device__ __forceinline__ float block_sum(float v, float *tmp)
-{
-    v = wave_sum(v);
-    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
-    __syncthreads();
-    const float t = (tmp[0] + tmp[1]) + (tmp[2] + tmp[3]);
-    __syncthreads();
-    return t;
-}
-__device__ __forceinline__ float block_max(float v, float *tmp)
-{
-    v = wave_max(v);
-    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
-    __syncthreads();
-    const float t = fmaxf(fmaxf(tmp[0], tmp[1]), fmaxf(tmp[2], tmp[3]));
-    __syncthreads();
-    return t;
-}
+// What a workgroup shares: the lanes' largest, then the waves' sums, and the candidates.
+template <int THREADS, uint32_t LIST>
+struct Shared {
+    uint32_t lanes[THREADS];
+    float2 sums[THREADS / 64];
+    uint32_t count;
+    uint64_t list[LIST];
+};
 
 struct PartArgs {
     psv_logprobs_args a;
@@ -100,102 +124,177 @@ struct PartArgs {
 // A record: M, sum e, sum e d, unused; the given tokens' logits (-infinity: not in this piece); the largest logits; their ids.
 __host__ __device__ inline uint32_t record_floats(uint32_t given, uint32_t top) { return 4 + given + 2 * top; }
 
+// A lane's E columns as they were read, 16-bit ones two to a register.
 template <uint32_t DT, int E>
-__global__ __launch_bounds__(kLogprobThreads) void k_logprobs_part(PartArgs g)
+struct Held {
+    static constexpr bool kHalves = DT != PSV_F32;
+    uint32_t w[kHalves ? E / 2 : E];
+    __device__ float get(int e) const
+    {
+        if constexpr (!kHalves) return __uint_as_float(w[e]);
+        else if constexpr (DT == PSV_BF16) return e & 1 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)(e & 1 ? w[e / 2] >> 16 : w[e / 2]));
+    }
+    // Columns 8 i to 8 i + 7
+    __device__ Held<DT, 8> group(uint32_t i) const
+    {
+        constexpr int GW = kHalves ? 4 : 8;
+        Held<DT, 8> h;
+#pragma unroll
+        for (int j = 0; j < GW; ++j) {
+            h.w[j] = w[j];
+#pragma unroll
+            for (int k = 1; k < E / 8; ++k) h.w[j] = i == (uint32_t)k ? w[k * GW + j] : h.w[j];
+        }
+        return h;
+    }
+    // Conversions are made again after this, not carried over in as many registers.
+    __device__ void forget()
+    {
+#pragma unroll
+        for (uint32_t &v : w) asm volatile("" : "+v"(v));
+    }
+};
+
+template <uint32_t DT, int E>
+__global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 64 ? 4 : 6) : (E == 64 ? 6 : 8)) void k_logprobs_part(PartArgs g)
 {
     using T = typename Elem<DT>::T;
-    constexpr int N = Elem<DT>::N;
-    struct __attribute__((packed, aligned(sizeof(T)))) Loose { Pack<DT, N> p; };      // rows of any alignment
-    __shared__ float tmp[kWaves];
-    __shared__ uint32_t lanes[kLogprobThreads + 1], count;
-    __shared__ uint2 list[kList];
+    constexpr int N = Elem<DT>::N, G = 8;
+    struct __attribute__((packed, aligned(sizeof(T)))) Loose { uint32_t w[4]; };      // rows of any alignment
+    __shared__ Shared<kThreads, kList> sh;
     const psv_logprobs_args &a = g.a;
     const uint32_t row = blockIdx.x / a.records, rec = blockIdx.x % a.records;
     const uint32_t c0 = min(rec * g.chunk, a.columns), c1 = min(c0 + g.chunk, a.columns);
     const T *px = static_cast<const T *>(a.logits) + (int64_t)row * a.row;
     float *out = g.records + (size_t)blockIdx.x * record_floats(a.given, a.top);
-    if (threadIdx.x < a.given) {
-        const int64_t t = (int64_t)a.tokens[(size_t)row * a.given + threadIdx.x] - a.first_token;
-        out[4 + threadIdx.x] = t >= c0 && t < c1 ? Elem<DT>::get(px[t]) : -INFINITY;
-    }
-    float x[E];
+    Held<DT, E> x;
 #pragma unroll
     for (int j = 0; j < E / N; ++j) {
         const uint32_t c = c0 + (j * kLogprobThreads + threadIdx.x) * N;
         if (c + N <= c1) {
-            const Pack<DT, N> p = reinterpret_cast<const Loose *>(px + c)->p;
+            const Loose p = *reinterpret_cast<const Loose *>(px + c);
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[j * N + e] = Elem<DT>::get(p.e[e]);
-        } else {
+            for (int i = 0; i < 4; ++i) x.w[j * 4 + i] = p.w[i];
+        } else {                                     // past the end of the piece: masked
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[j * N + e] = c + e < c1 ? Elem<DT>::get(px[c + e]) : -INFINITY;
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (DT == PSV_F32) {
+                    x.w[j * 4 + i] = c + i < c1 ? __float_as_uint(px[c + i]) : 0xff800000u;
+                } else {
+                    const uint16_t *ph = reinterpret_cast<const uint16_t *>(px);
+                    const uint32_t none = DT == PSV_BF16 ? 0xff80u : 0xfc00u;
+                    const uint32_t lo = c + 2 * i < c1 ? ph[c + 2 * i] : none, hi = c + 2 * i + 1 < c1 ? ph[c + 2 * i + 1] : none;
+                    x.w[j * 4 + i] = lo | hi << 16;
+                }
+            }
         }
     }
-    float mine = -INFINITY;
+    if (threadIdx.x < a.given) {
+        const int64_t t = (int64_t)a.tokens[(size_t)row * a.given + threadIdx.x] - a.first_token;
+        out[4 + threadIdx.x] = t >= c0 && t < c1 ? Elem<DT>::get(px[t]) : -INFINITY;
+    }
+    // the largest of every group of eight columns, of the lane, and -- with the bound of the alternatives -- of the workgroup
+    float most[E / G], mine = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < E; ++e) mine = fmaxf(mine, x[e]);
-    const float M = block_max(mine, tmp), ref = M == -INFINITY ? 0.f : M;
+    for (int i = 0; i < E / G; ++i) {
+        float m = x.get(i * G);
+#pragma unroll
+        for (int e = 1; e < G; ++e) m = __builtin_elementwise_maximum(m, x.get(i * G + e));
+        most[i] = m;
+        mine = __builtin_elementwise_maximum(mine, m);
+    }
+    sh.lanes[threadIdx.x] = order_of(mine);
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    uint32_t w4[kWaves], top_order = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        w4[i] = sh.lanes[i * 64 + (threadIdx.x & 63)];
+        top_order = max(top_order, w4[i]);
+    }
+    top_order = wave_max_u32(top_order);
+    const bool bad = top_order >= kOrderInf;          // a NaN or +infinity
+    const float M = of_order(top_order), ref = top_order == kOrderNone ? 0.f : M;
     float s = 0.f, w = 0.f;
+    x.forget();
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float d = x[e] - ref, p = exp2_raw(d * g.to_log2);
+        const float d = fmaxf(x.get(e) - ref, kLowest), p = exp2_raw(d * g.to_log2);      // a masked logit: p = 0 and a finite d
         s += p;
-        w = fmaf(p, p > 0.f ? d : 0.f, w);      // a masked logit has no part
+        w = fmaf(p, d, w);
     }
-    s = block_sum(s, tmp);
-    w = block_sum(w, tmp);
-    if (threadIdx.x == 0) {
-        out[0] = M;
-        out[1] = s;
-        out[2] = w;
-        out[3] = 0.f;
-    }
-    if (a.top == 0) return;
-
+    s = wave_sum(s);
+    w = wave_sum(w);
+    if ((threadIdx.x & 63) == 0) sh.sums[threadIdx.x >> 6] = make_float2(s, w);
     float *values = out + 4 + a.given;
     int32_t *ids = reinterpret_cast<int32_t *>(values + a.top);
-    if (!(s == s)) {                            // a NaN or +infinity: no alternatives
-        write_ranked(list, 0, a.top, values, ids);
-        return;
-    }
-    auto id_of = [&](int e) { return c0 + ((e / N) * kLogprobThreads + threadIdx.x) * N + e % N; };
-    uint32_t bound = kth_largest(order_of(mine), a.top, lanes);
-    if (bound <= kOrderNone) bound = kOrderNone + 1;
-    const float least = of_order(bound);
-    uint32_t last = ~0u;                        // highest id taken of those equal to `least`
-    for (int pass = 0;; ++pass) {
-        if (threadIdx.x == 0) count = 0;
+    uint32_t n = 0;
+    if (a.top == 0 || bad) {
         __syncthreads();
-        if (mine >= least) {
+    } else {
+        const float least = of_order(max(kth_largest<DT == PSV_F32 ? 0 : DT == PSV_BF16 ? 16 : 13>(w4, a.top, enough_lanes(a.top, a.top / 2, kList / E)), kOrderNone + 1));
+        uint32_t last = ~0u;                        // highest id taken of those equal to `least`
+        uint32_t groups = 0;                        // the few that reach it are looked through one by one
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (x[e] >= least) {
-                    const uint32_t id = id_of(e);
-                    if (x[e] > least || id <= last) {
-                        const uint32_t at = atomicAdd(&count, 1u);
-                        if (at < kList) list[at] = make_uint2(order_of(x[e]), id);
-                    }
-                }
-        }
-        __syncthreads();
-        if (count <= kList || pass) break;
-        // too many equal ones: those lanes that exceed the bound count first, then the lanes by their first id
-        uint32_t key = 0;
-        if (mine > least) key = ~0u;
-        else if (mine == least) {
-            uint32_t first = ~0u;
+        for (int i = 0; i < E / G; ++i) groups |= most[i] >= least ? 1u << i : 0u;
+        auto id_of = [&](uint32_t i, uint32_t e) { return c0 + threadIdx.x * N + i * (G * kThreads) + e / N * (kThreads * N) + e % N; };
+        x.forget();
+        for (int pass = 0;; ++pass) {
+            for (uint32_t left = groups; left; left &= left - 1) {
+                const uint32_t i = __builtin_ctz(left);
+                const Held<DT, G> h = x.group(i);
+                uint32_t hits = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (x[e] == least) first = min(first, id_of(e));
-            key = ~first;
+                for (int e = G - 1; e >= 0; --e) hits = 2 * hits + (h.get(e) >= least);
+                if (pass)
+#pragma unroll
+                    for (int e = 0; e < G; ++e)
+                        if (h.get(e) == least && id_of(i, e) > last) hits &= ~(1u << e);
+                uint32_t at = list_places(&sh.count, (uint32_t)__popc(hits));
+#pragma unroll
+                for (int e = 0; e < G; ++e)
+                    if ((hits >> e & 1) && at < kList) sh.list[at++] = list_entry(order_of(h.get(e)), id_of(i, e));
+            }
+            __syncthreads();
+            n = sh.count;
+            if (n <= kList) break;
+            if (pass) { n = kList; break; }         // not reached: no read behind the list all the same
+            // too many equal ones: those lanes that exceed the bound count first, then the lanes by their first id
+            uint32_t key = 0;
+            if (mine > least) {
+                key = ~0u;
+            } else if (groups) {
+                const uint32_t i = __builtin_ctz(groups);
+                const Held<DT, G> h = x.group(i);
+#pragma unroll
+                for (int e = G - 1; e >= 0; --e)
+                    if (h.get(e) == least) key = ~id_of(i, e);
+            }
+            sh.lanes[threadIdx.x] = key;
+            __syncthreads();
+            if (threadIdx.x == 0) sh.count = 0;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) w4[i] = sh.lanes[i * 64 + (threadIdx.x & 63)];
+            last = ~kth_largest<0>(w4, a.top, a.top);
+            __syncthreads();
         }
-        __syncthreads();
-        last = ~kth_largest(key, a.top, lanes);
+        rank_list<kThreads>(sh.list, n, a.top, [&](uint32_t rank, uint64_t v) {
+            values[rank] = entry_value(v);
+            ids[rank] = (int32_t)(entry_id(v) + a.first_token);
+        });
     }
-    const uint32_t n = min(count, kList);
-    for (uint32_t i = threadIdx.x; i < n; i += kLogprobThreads) list[i].y += a.first_token;
-    __syncthreads();
-    write_ranked(list, n, a.top, values, ids);
+    for (uint32_t i = n + threadIdx.x; i < a.top; i += kLogprobThreads) {
+        values[i] = -INFINITY;
+        ids[i] = -1;
+    }
+    if (threadIdx.x == 0) {
+        const float2 a0 = sh.sums[0], a1 = sh.sums[1], a2 = sh.sums[2], a3 = sh.sums[3];
+        out[0] = M;
+        out[1] = bad ? nan32() : (a0.x + a1.x) + (a2.x + a3.x);
+        out[2] = (a0.y + a1.y) + (a2.y + a3.y);
+        out[3] = 0.f;
+    }
 }
 
 template <uint32_t DT>
@@ -222,83 +321,165 @@ struct JoinArgs {
     const float *records;   // [shards][rows][records] of them
     uint32_t shards;
     psv_logprobs_out out;
+    uint32_t by_top, by_records;      // divisions as products: i / top = i * by_top >> 21 for i < 256 top, k / records = k * by_records >> 16 for k < 256
 };
 
-__global__ __launch_bounds__(kLogprobThreads) void k_logprobs_join(JoinArgs g)
+// One workgroup a row.  64 threads, where a row has no more records than those and at most kHeld alternatives a lane: a
+// wave needs no barriers, and a compute unit has room for as many rows as it has wave slots.  (8 records of 8 alternatives, 2048
+// rows: 6.4 us, with 256 threads 13.4.)
+constexpr uint32_t kHeld = 8;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_logprobs_join(JoinArgs g)
 {
-    __shared__ float tmp[kWaves], values[PSV_LOGPROBS_MAX_TOP];
-    __shared__ int32_t ids[PSV_LOGPROBS_MAX_TOP];
-    __shared__ uint32_t lanes[kLogprobThreads + 1], count;
-    __shared__ uint2 list[kList];
+    constexpr int W = THREADS / 64;
+    constexpr uint32_t LIST = THREADS == 64 ? PSV_LOGPROBS_MAX_TOP * kHeld : kList;
+    __shared__ Shared<THREADS, LIST> sh;
+    __shared__ float given_s[PSV_LOGPROBS_MAX_GIVEN];
+    __shared__ uint32_t most_s[W];
     const psv_logprobs_args &a = g.a;
     const uint32_t row = blockIdx.x, size = record_floats(a.given, a.top), n_rec = g.shards * a.records;
-    auto record = [&](uint32_t i) { return g.records + (((size_t)(i / a.records) * a.rows + row) * a.records + i % a.records) * size; };
-    float m = -INFINITY, s = 0.f, w = 0.f;
+    auto record = [&](uint32_t k) {
+        const uint32_t shard = k * g.by_records >> 16;
+        return g.records + ((size_t)(shard * (a.rows - 1) + row) * a.records + k) * size;      // ((shard * rows + row) * records + k - shard * records)
+    };
+    float m = -INFINITY, s = 0.f, w = 0.f, x0 = -INFINITY;
     if (threadIdx.x < n_rec) {
         const float *r = record(threadIdx.x);
         m = r[0];
         s = r[1];
         w = r[2];
+        if (a.given) x0 = r[4];
     }
-    const float M = block_max(m, tmp);
-    if (m > -INFINITY || s != s) {
+    // The alternatives of all records; a wave keeps its lanes' in registers.  Ids differ, so that an (order, id) is held by one lane.
+    const uint32_t n_all = g.out.top_ids ? n_rec * a.top : 0;
+    auto entry = [&](uint32_t i) {
+        const uint32_t k = i * g.by_top >> 21;
+        const float *r = record(k) + 4 + a.given + (i - k * a.top);
+        return make_uint2(THREADS == 64 ? __float_as_uint(r[0]) : order_of(r[0]), __float_as_uint(r[a.top]));
+    };
+    uint2 held[kHeld];
+    if constexpr (THREADS == 64)
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {          // all requested at once; their orders are made when they have arrived
+            held[j] = make_uint2(0, 0);
+            if (j * THREADS < n_all) held[j] = entry(min(j * THREADS + threadIdx.x, n_all - 1));
+        }
+    uint2 best = make_uint2(0, 0);
+    auto look = [&](uint2 v) {
+        if (v.x > best.x || (v.x == best.x && v.y < best.y)) best = v;
+    };
+    if constexpr (THREADS == 64) {
+        if (n_all)
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            held[j].x = j * THREADS + threadIdx.x < n_all ? order_of(__uint_as_float(held[j].x)) : 0;
+            look(held[j]);
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < n_all; i += THREADS) look(entry(i));
+    }
+    static_assert(PSV_LOGPROBS_MAX_GIVEN <= THREADS && PSV_LOGPROBS_MAX_TOP <= THREADS, "one lane each");
+    if (threadIdx.x < PSV_LOGPROBS_MAX_GIVEN) given_s[threadIdx.x] = -INFINITY;
+    if (threadIdx.x == 0) sh.count = 0;
+    sh.lanes[threadIdx.x] = best.x;
+    const uint32_t most = wave_max_u32(s != s ? ~0u : order_of(m));
+    if ((threadIdx.x & 63) == 0) most_s[threadIdx.x >> 6] = most;
+    __syncthreads();
+    uint32_t top_order = most_s[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) top_order = max(top_order, most_s[i]);
+    const bool bad = top_order >= kOrderInf;
+    const float M = of_order(top_order);
+    // a given token's logit lies in one record
+    if (x0 > -INFINITY) given_s[0] = x0;
+    if (threadIdx.x < n_rec)
+        for (uint32_t k = 1; k < a.given; ++k) {
+            const float x = record(threadIdx.x)[4 + k];
+            if (x > -INFINITY) given_s[k] = x;
+        }
+    if (m > -INFINITY) {
         const float d = m - M, f = exp2_raw(d * a.scale * 1.4426950408889634f);
         w = f * (w + (f > 0.f ? s * d : 0.f));
         s *= f;
     }
-    const float S = block_sum(s, tmp), W = block_sum(w, tmp);
-    const bool bad = !(S == S), none = S == 0.f;
+    s = wave_sum(s);
+    w = wave_sum(w);
+    if ((threadIdx.x & 63) == 0) sh.sums[threadIdx.x >> 6] = make_float2(s, w);
+    uint32_t n = 0;
+    if (n_all == 0 || bad) {
+        __syncthreads();
+    } else {
+        uint32_t w4[W], last = ~0u;
+#pragma unroll
+        for (int i = 0; i < W; ++i) w4[i] = sh.lanes[i * 64 + (threadIdx.x & 63)];
+        const uint32_t bound = max(kth_largest<0>(w4, a.top, enough_lanes(a.top, a.top / 4, LIST / (THREADS == 64 ? kHeld : 32))), kOrderNone + 1);
+        for (int pass = 0;; ++pass) {
+            auto reaches = [&](uint2 v) { return v.x > bound || (v.x == bound && v.y <= last); };
+            if constexpr (THREADS == 64) {          // the wave's places by counting: nothing to wait for
+                n = 0;
+#pragma unroll
+                for (int j = 0; j < kHeld; ++j) {
+                    const bool hit = reaches(held[j]);
+                    const uint64_t hits = __ballot(hit);
+                    const uint32_t at = __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, n));
+                    if (hit && at < LIST) sh.list[at] = list_entry(held[j].x, held[j].y);
+                    n += __popcll(hits);
+                }
+                __syncthreads();
+            } else {
+                for (uint32_t i = threadIdx.x; i < n_all; i += THREADS) {
+                    const uint2 v = entry(i);
+                    if (!reaches(v)) continue;
+                    const uint32_t at = list_places(&sh.count, 1);
+                    if (at < LIST) sh.list[at] = list_entry(v.x, v.y);
+                }
+                __syncthreads();
+                n = sh.count;
+            }
+            if (n <= LIST) break;
+            if (pass) { n = LIST; break; }
+            sh.lanes[threadIdx.x] = best.x > bound ? ~0u : best.x == bound ? ~best.y : 0u;
+            __syncthreads();
+            if (threadIdx.x == 0) sh.count = 0;
+#pragma unroll
+            for (int i = 0; i < W; ++i) w4[i] = sh.lanes[i * 64 + (threadIdx.x & 63)];
+            last = ~kth_largest<0>(w4, a.top, a.top);
+            __syncthreads();
+        }
+    }
+    float S = 0.f, D = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        S += sh.sums[i].x;
+        D += sh.sums[i].y;
+    }
     const float ln_s = logf(S);
-    auto answer = [&](float x) { return bad ? __uint_as_float(0x7fc00000u) : none || x == -INFINITY ? -INFINITY : (x - M) * a.scale - ln_s; };
-    if (g.out.entropy && threadIdx.x == 0) g.out.entropy[row] = bad ? __uint_as_float(0x7fc00000u) : none ? 0.f : ln_s - W * a.scale / S;
+    const bool none = top_order == kOrderNone;
+    auto answer = [&](float x) { return bad ? nan32() : none || x == -INFINITY ? -INFINITY : (x - M) * a.scale - ln_s; };
+    if (g.out.entropy && threadIdx.x == 0) g.out.entropy[row] = bad ? nan32() : none ? 0.f : ln_s - D * a.scale / S;
     if (g.out.logprobs && threadIdx.x < a.given) {
         const int32_t t = a.tokens[(size_t)row * a.given + threadIdx.x];
-        float x = -INFINITY;
-        for (uint32_t i = 0; i < n_rec; ++i) x = fmaxf(x, record(i)[4 + threadIdx.x]);
-        g.out.logprobs[(size_t)row * a.given + threadIdx.x] = t < 0 ? 0.f : (uint32_t)t >= a.vocab ? __uint_as_float(0x7fc00000u) : answer(x);
+        g.out.logprobs[(size_t)row * a.given + threadIdx.x] = t < 0 ? 0.f : (uint32_t)t >= a.vocab ? nan32() : answer(given_s[threadIdx.x]);
     }
-    if (!g.out.top_ids || a.top == 0) return;
-    const uint32_t n_all = bad ? 0 : n_rec * a.top;
-    auto entry = [&](uint32_t i, uint2 &v) {
-        const float *r = record(i / a.top) + 4 + a.given + i % a.top;
-        v = make_uint2(order_of(r[0]), __float_as_uint(r[a.top]));
-    };
-    // the lanes' largest, then all that reach the top-th of them: ids differ, so that an (order, id) is held by one
-    uint2 v, best = make_uint2(0, 0);
-    for (uint32_t i = threadIdx.x; i < n_all; i += kLogprobThreads) {
-        entry(i, v);
-        if (v.x > best.x || (v.x == best.x && v.y < best.y)) best = v;
-    }
-    uint32_t bound = kth_largest(best.x, a.top, lanes), last = ~0u;
-    if (bound <= kOrderNone) bound = kOrderNone + 1;
-    for (int pass = 0;; ++pass) {
-        if (threadIdx.x == 0) count = 0;
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < n_all; i += kLogprobThreads) {
-            entry(i, v);
-            if (v.x > bound || (v.x == bound && v.y <= last)) {
-                const uint32_t at = atomicAdd(&count, 1u);
-                if (at < kList) list[at] = v;
-            }
-        }
-        __syncthreads();
-        if (count <= kList || pass) break;
-        const uint32_t key = best.x > bound ? ~0u : best.x == bound ? ~best.y : 0u;
-        __syncthreads();
-        last = ~kth_largest(key, a.top, lanes);
-    }
-    write_ranked(list, min(count, kList), a.top, values, ids);
-    __syncthreads();
-    if (threadIdx.x < a.top) {
-        g.out.top_ids[(size_t)row * a.top + threadIdx.x] = ids[threadIdx.x];
-        g.out.top_logprobs[(size_t)row * a.top + threadIdx.x] = bad ? __uint_as_float(0x7fc00000u) : answer(values[threadIdx.x]);
+    if (!g.out.top_ids) return;
+    int32_t *ids = g.out.top_ids + (size_t)row * a.top;
+    float *values = g.out.top_logprobs + (size_t)row * a.top;
+    rank_list<THREADS>(sh.list, n, a.top, [&](uint32_t rank, uint64_t v) {
+        ids[rank] = (int32_t)entry_id(v);
+        values[rank] = answer(entry_value(v));
+    });
+    for (uint32_t i = n + threadIdx.x; i < a.top; i += THREADS) {
+        ids[i] = -1;
+        values[i] = bad ? nan32() : -INFINITY;
     }
 }
 
 hipError_t launch_logprobs_join(const psv_logprobs_args &a, const float *records, uint32_t shards, const psv_logprobs_out &out, hipStream_t s)
 {
-    const JoinArgs g{a, records, shards, out};
-    PSV_LAUNCH(k_logprobs_join, dim3(a.rows), dim3(kLogprobThreads), 0, s, g);
+    const JoinArgs g{a, records, shards, out, a.top ? ((1u << 21) + a.top - 1) / a.top : 0, (65536 + a.records - 1) / a.records};
+    const uint32_t n = shards * a.records;
+    if (n <= 64 && n * a.top <= 64 * kHeld) PSV_LAUNCH(k_logprobs_join<64>, dim3(a.rows), dim3(64), 0, s, g);
+    else PSV_LAUNCH(k_logprobs_join<kThreads>, dim3(a.rows), dim3(kThreads), 0, s, g);
     return hipGetLastError();
 }
 

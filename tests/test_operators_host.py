@@ -207,7 +207,7 @@ def logprob_args(**kw):
 
 
 SHARED = [dict(tokens=None), dict(tokens=2 * P + 1), dict(rows=(1 << 20) + 1), dict(given=33), dict(top=33), dict(scale=0.0), dict(scale=-1.0),
-          dict(scale=float("nan")), dict(scale=float("inf")), dict(vocab=0), dict(vocab=(1 << 21) + 1)]
+          dict(scale=float("nan")), dict(scale=1e-10), dict(scale=5e9), dict(scale=float("inf")), dict(vocab=0), dict(vocab=(1 << 21) + 1)]
 
 
 @pytest.mark.parametrize("kw", SHARED + [dict(logits=None), dict(logits=P + 2), dict(columns=0), dict(columns=(1 << 21) + 1), dict(first_token=1), dict(vocab=999),
