@@ -126,7 +126,7 @@ psv_status psv_cache_slots(const psv_slots_args *a, void *stream);
 
 /* ---- rows into and out of the cache ------------------------------------------------------------- */
 
-/* One layer's pools (preserve.h, KV-cache) */
+/* One layer's pools (preserve.h, KV-cache).  Of a call, rows * n_kv_heads <= 2^28 (else PSV_ERR_UNSUPPORTED). */
 typedef struct {
     void *k_pool, *v_pool;        /* dev, 16-byte aligned */
     uint32_t n_kv_heads;          /* 1 .. 128 */

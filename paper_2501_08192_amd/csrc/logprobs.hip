@@ -30,16 +30,6 @@ constexpr float kLowest = -3.402823466e38f;
 
 __device__ __forceinline__ float nan32() { return __uint_as_float(0x7fc00000u); }
 
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
-{
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));
-    const uint32_t a = max((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16));
-    return max(a, max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48)));
-}
-
 // The k-th largest of the workgroup's values (k <= threads), or a lower one that at most `enough` of them reach: bit by bit, from the first
 // in which the largest and the smallest differ down to bit LOW (below it an order has zeros, or ones where the value is negative).  A wave has
 // all of them, one of each wave a lane, and counts for itself.  Bound by the way from the comparisons to the scalar unit and back, some

@@ -10,7 +10,7 @@ using namespace psv;
 namespace {
 
 constexpr double kPi = 3.14159265358979323846;
-constexpr uint32_t kMostRows = 1u << 24;      // of a call: what a grid of whole workgroups can name
+constexpr uint32_t kMostRows = 1u << 24, kMostHeads = 1u << 28;      // rows, and kv heads of all rows, of a call: what a grid of whole workgroups can name
 
 size_t elem_size(uint32_t dtype) { return dtype == PSV_F32 ? 4 : 2; }
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -181,6 +181,7 @@ psv_status psv_cache_append(const psv_append_args *a, const psv_cache *cache, co
     if (!a || !cache || !cache_ok(*cache) || (rope && !rope_ok(*rope))) return PSV_ERR_INVALID_ARG;
     if (a->rows > kMostRows || a->n_q_heads > 128 || a->dtype > PSV_F16) return PSV_ERR_INVALID_ARG;
     if (rope && (rope->dims > PSV_HEAD_DIM || rope->dims % 16)) return PSV_ERR_UNSUPPORTED;
+    if ((uint64_t)a->rows * cache->n_kv_heads > kMostHeads) return PSV_ERR_UNSUPPORTED;
     if (a->rows == 0) return PSV_OK;
     if (!a->slots || !aligned(a->slots, 8) || (rope && !a->positions) || !aligned(a->positions, 4)) return PSV_ERR_INVALID_ARG;
     if (!rows_ok(a->k, a->k_row, cache->n_kv_heads, a->dtype, a->rows, false) || !rows_ok(a->v, a->v_row, cache->n_kv_heads, a->dtype, a->rows, false)) return PSV_ERR_INVALID_ARG;
@@ -194,6 +195,7 @@ psv_status psv_cache_append(const psv_append_args *a, const psv_cache *cache, co
 psv_status psv_cache_gather(const psv_gather_args *a, const psv_cache *cache, void *stream)
 {
     if (!a || !cache || !cache_ok(*cache) || a->rows > kMostRows || a->dtype > PSV_F16) return PSV_ERR_INVALID_ARG;
+    if ((uint64_t)a->rows * cache->n_kv_heads > kMostHeads) return PSV_ERR_UNSUPPORTED;
     if (a->rows == 0) return PSV_OK;
     if (!a->slots || !aligned(a->slots, 8)) return PSV_ERR_INVALID_ARG;
     if (!rows_ok(a->k, a->k_row, cache->n_kv_heads, a->dtype, a->rows, true) || !rows_ok(a->v, a->v_row, cache->n_kv_heads, a->dtype, a->rows, true)) return PSV_ERR_INVALID_ARG;

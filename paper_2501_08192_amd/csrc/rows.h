@@ -32,15 +32,25 @@ template <> struct Elem<PSV_F16> {
 template <uint32_t DT, int N>
 struct Pack { typename Elem<DT>::T e[N]; };
 
-// N adjacent elements, in one load or store of 16 (or 8) bytes where N is that many.
+// N adjacent elements, in one load or store of 16 (or 8) bytes where N is that many.  A load and its conversion apart: kernels request the rows of
+// their next step before they work on this one's.
 template <uint32_t DT, int N>
-__device__ __forceinline__ void load_row(const typename Elem<DT>::T *p, float (&v)[N])
+__device__ __forceinline__ Pack<DT, N> fetch_row(const typename Elem<DT>::T *p)
 {
     using P = Pack<DT, N>;
     struct alignas(sizeof(P) > 16 ? 16 : sizeof(P)) A { P p; };
-    const P t = reinterpret_cast<const A *>(p)->p;
+    return reinterpret_cast<const A *>(p)->p;
+}
+template <uint32_t DT, int N>
+__device__ __forceinline__ void unpack_row(const Pack<DT, N> &t, float (&v)[N])
+{
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = Elem<DT>::get(t.e[e]);
+}
+template <uint32_t DT, int N>
+__device__ __forceinline__ void load_row(const typename Elem<DT>::T *p, float (&v)[N])
+{
+    unpack_row<DT, N>(fetch_row<DT, N>(p), v);
 }
 template <uint32_t DT, int N>
 __device__ __forceinline__ void store_row(typename Elem<DT>::T *p, const float (&v)[N])
@@ -88,6 +98,17 @@ __device__ __forceinline__ float2 turn(double angle, double magnitude)
     const long long q = (long long)k;
     const double cc = (q & 1) ? s : c, ss = (q & 1) ? c : s;
     return make_float2((float)(((q + 1) & 2) ? -cc * magnitude : cc * magnitude), (float)((q & 2) ? -ss * magnitude : ss * magnitude));
+}
+
+// Maximum over the 64 lanes of a wave, returned in every lane (all lanes must be active).
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));
+    const uint32_t a = max((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16));
+    return max(a, max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48)));
 }
 
 // Pairs (a, b) turned: a' = a c - b s, b' = b c + a s.

@@ -177,6 +177,7 @@ def test_append_refuses(kw):
 
 def test_append_unsupported_rotations_and_no_rows():
     assert append_status(rope_kw=dict(dims=256)) == UNSUPPORTED and append_status(rope_kw=dict(dims=72)) == UNSUPPORTED
+    assert append_status(rows=1 << 24, cache_kw=dict(n_kv_heads=17)) == UNSUPPORTED
     assert append_status(rows=0, k=None, v=None, slots=None) == psv.PSV_OK
     assert psv.lib().psv_cache_append(None, None, None, None) == BAD
 
