@@ -429,23 +429,37 @@ def psv_debug_force_wait_timeout(ctx, on):
 # ---- operators around the decode step (include/preserve_ops.h) -----------------------------------------------------------
 
 
-def _rows(name, t):
-    """(dtype code, row stride) of rows [rows, heads, channels] whose heads and channels are adjacent."""
-    if t.dim() != 3 or t.shape[2] != 128 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != 128):
-        raise ValueError("%s: rows of [heads][128] adjacent elements are wanted, got shape %s, strides %s" % (name, tuple(t.shape), t.stride()))
-    return _dtype(name, t), t.stride(0)
+_TYPES = {}      # a tensor's dtype -> its name; filled as types are seen
+
+
+def _type(t):
+    name = _TYPES.get(t.dtype)
+    if name is None:
+        name = _TYPES[t.dtype] = str(t.dtype).replace("torch.", "")
+    return name
+
+
+_ROW_TYPES = {"float32": PSV_F32, "bfloat16": PSV_BF16, "float16": PSV_F16}
 
 
 def _dtype(name, t):
-    code = {"torch.float32": PSV_F32, "torch.bfloat16": PSV_BF16, "torch.float16": PSV_F16}.get(str(t.dtype))
+    code = _ROW_TYPES.get(_type(t))
     if code is None:
         raise ValueError("%s: float32, bfloat16 or float16 is wanted, got %s" % (name, t.dtype))
     return code
 
 
+def _rows(name, t):
+    """(dtype code, row stride, shape) of rows [rows, heads, channels] whose heads and channels are adjacent."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or (shape[1] > 1 and stride[1] != 128):
+        raise ValueError("%s: rows of [heads][128] adjacent elements are wanted, got shape %s, strides %s" % (name, tuple(shape), stride))
+    return _dtype(name, t), stride[0], shape
+
+
 def _want(name, t, dtype, *shape):
-    """A contiguous tensor of a type and shape; None where an axis may have any length."""
-    if str(t.dtype) != "torch." + dtype or not t.is_contiguous() or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+    """The address of a contiguous tensor of a type and shape."""
+    if _type(t) != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: contiguous %s %s is wanted, got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
     return t.data_ptr()
 
@@ -465,11 +479,11 @@ def psv_set_rope(ctx, rope):
 
 def psv_rotate(x, y, positions, rope, stream, transpose=False):
     """x, y: [rows, heads, channels] of one type, any strides with adjacent channels; positions: int32 [rows]."""
-    rows, heads, dim = x.shape
-    if y.shape != x.shape or y.dtype != x.dtype or (dim > 1 and (x.stride(2) != 1 or y.stride(2) != 1)):
-        raise ValueError("psv_rotate: x and y of one shape and type with adjacent channels are wanted")
-    a = psv_rotate_args(x.data_ptr(), y.data_ptr(), _want("positions", positions, "int32", rows), rows, heads, dim, _dtype("x", x),
-                        1 if transpose else 0, 0, x.stride(0), x.stride(1), y.stride(0), y.stride(1))
+    shape, xs, ys = x.shape, x.stride(), y.stride()
+    if len(shape) != 3 or y.shape != shape or y.dtype != x.dtype or (shape[2] > 1 and (xs[2] != 1 or ys[2] != 1)):
+        raise ValueError("psv_rotate: x and y of one shape [rows, heads, channels] and type with adjacent channels are wanted")
+    a = psv_rotate_args(x.data_ptr(), y.data_ptr(), _want("positions", positions, "int32", shape[0]), shape[0], shape[1], shape[2], _dtype("x", x),
+                        1 if transpose else 0, 0, xs[0], xs[1], ys[0], ys[1])
     _check(lib().psv_rotate(C.byref(a), C.byref(rope), _stream(stream)), "psv_rotate")
 
 
@@ -479,12 +493,11 @@ def psv_cache_slots(lens, new_lens, block_table, free_blocks, free_range, num_po
     for a contiguous cache."""
     n, rows = lens.shape[0], slots.shape[0]
     table = block_table is not None
-    mb = block_table.shape[1] if table else int(max_blocks)
+    mb, n_free = (block_table.shape[-1], free_blocks.shape[0]) if table else (int(max_blocks), 0)
     a = psv_slots_args(_want("lens", lens, "int32", n), _want("new_lens", new_lens, "int32", n),
-                       _want("block_table", block_table, "int32", n, None) if table else None,
-                       _want("free_blocks", free_blocks, "int32", None) if table else None,
-                       _want("free_range", free_range, "int32", 2) if table else None, free_blocks.shape[0] if table else 0, n, mb,
-                       num_pool_blocks, rows, 0, _want("seq_lens", seq_lens, "int32", n), _want("row_starts", row_starts, "int32", n + 1),
+                       _want("block_table", block_table, "int32", n, mb) if table else None,
+                       _want("free_blocks", free_blocks, "int32", n_free) if table else None,
+                       _want("free_range", free_range, "int32", 2) if table else None, n_free, n, mb, num_pool_blocks, rows, 0, _want("seq_lens", seq_lens, "int32", n), _want("row_starts", row_starts, "int32", n + 1),
                        _want("slots", slots, "int64", rows), _want("positions", positions, "int32", rows),
                        _want("requests", requests, "int32", rows), _want("free_range_out", free_range_out, "int32", 2) if table else None,
                        _want("refused", refused, "int32", 1))
@@ -498,28 +511,28 @@ def kv_cache(k_pool, v_pool, n_kv_heads, kv_format, kv_layout, num_pool_blocks):
 
 def psv_cache_append(q, k, v, q_out, positions, slots, cache, rope, stream):
     """q, q_out [rows, q heads, 128], or None; k, v [rows, kv heads, 128]; positions int32 [rows] (None without rope); slots int64 [rows]."""
-    rows = k.shape[0]
-    dt, k_row = _rows("k", k)
-    dv, v_row = _rows("v", v)
-    if dv != dt or v.shape != k.shape or k.shape[1] != cache.n_kv_heads:
+    dt, k_row, shape = _rows("k", k)
+    dv, v_row, v_shape = _rows("v", v)
+    if dv != dt or v_shape != shape or shape[1] != cache.n_kv_heads:
         raise ValueError("psv_cache_append: k and v of one type with the cache's %d heads are wanted" % cache.n_kv_heads)
-    nq = q_row = q_out_row = 0
+    rows, nq, q_row, q_out_row, q_at, q_out_at = shape[0], 0, 0, 0, None, None
     if q is not None:
-        (dq, q_row), (do, q_out_row), nq = _rows("q", q), _rows("q_out", q_out), q.shape[1]
-        if dq != dt or do != dt or q_out.shape != q.shape or q.shape[0] != rows:
+        dq, q_row, q_shape = _rows("q", q)
+        do, q_out_row, q_out_shape = _rows("q_out", q_out)
+        if dq != dt or do != dt or q_out_shape != q_shape or q_shape[0] != rows:
             raise ValueError("psv_cache_append: q and q_out of k's type and rows are wanted")
-    a = psv_append_args(_dev_ptr(q), k.data_ptr(), v.data_ptr(), None if q is None else q_out.data_ptr(),
-                        None if positions is None else _want("positions", positions, "int32", rows), _want("slots", slots, "int64", rows),
-                        rows, nq, dt, 0, q_row, k_row, v_row, q_out_row)
+        nq, q_at, q_out_at = q_shape[1], q.data_ptr(), q_out.data_ptr()
+    a = psv_append_args(q_at, k.data_ptr(), v.data_ptr(), q_out_at, None if positions is None else _want("positions", positions, "int32", rows),
+                        _want("slots", slots, "int64", rows), rows, nq, dt, 0, q_row, k_row, v_row, q_out_row)
     _check(lib().psv_cache_append(C.byref(a), C.byref(cache), None if rope is None else C.byref(rope), _stream(stream)), "psv_cache_append")
 
 
 def psv_cache_gather(slots, k, v, cache, stream):
     """slots int64 [rows]; k, v [rows, kv heads, 128] of one type."""
     rows = slots.shape[0]
-    dt, k_row = _rows("k", k)
-    dv, v_row = _rows("v", v)
-    if dv != dt or v.shape != k.shape or k.shape[0] != rows or k.shape[1] != cache.n_kv_heads:
+    dt, k_row, shape = _rows("k", k)
+    dv, v_row, v_shape = _rows("v", v)
+    if dv != dt or v_shape != shape or shape[0] != rows or shape[1] != cache.n_kv_heads:
         raise ValueError("psv_cache_gather: k and v of one type with %d rows of the cache's %d heads are wanted" % (rows, cache.n_kv_heads))
     a = psv_gather_args(_want("slots", slots, "int64", rows), k.data_ptr(), v.data_ptr(), rows, dt, k_row, v_row)
     _check(lib().psv_cache_gather(C.byref(a), C.byref(cache), _stream(stream)), "psv_cache_gather")
@@ -537,9 +550,10 @@ def _logprobs_args(rows, logits, tokens, scale, top, first_token, vocab, records
     given = 0 if tokens is None else tokens.shape[1]
     columns, row, dt = 0, 0, PSV_F32
     if logits is not None:
-        if logits.dim() != 2 or logits.shape[0] != rows or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        shape, stride = logits.shape, logits.stride()
+        if len(shape) != 2 or shape[0] != rows or (shape[1] > 1 and stride[1] != 1):
             raise ValueError("logits: [rows, columns] with adjacent columns are wanted")
-        columns, row, dt = logits.shape[1], max(logits.stride(0), logits.shape[1]) if rows == 1 else logits.stride(0), _dtype("logits", logits)
+        columns, row, dt = shape[1], stride[0], _dtype("logits", logits)
     return psv_logprobs_args(_dev_ptr(logits), None if given == 0 else _want("tokens", tokens, "int32", rows, given), rows, columns, first_token,
                              columns if vocab is None else vocab, dt, given, top, scale, records, 0, row)
 
