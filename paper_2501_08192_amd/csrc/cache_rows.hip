@@ -5,12 +5,14 @@
 // of 128 lines.  Its rows go through LDS, and where eight of them follow one another from a slot that is a multiple of eight on -- all of a
 // prompt but its ends -- a lane moves one channel of the eight at once.  Such an octet belongs to the workgroup that has its first row, so that
 // where tiles of rows end does not matter.  The two kinds of work are workgroups of their own, side by side in one launch.
+// (Append of 9500 rows of 8 query and 2 kv heads, 58 MB: 11.5 us, 5.1 TB/s, with two-byte stores of values 22.6; of 3072 rows of 16 and 2 into an
+// int8 cache, 30 MB: 9.7 us; gather of 24400 rows of 2 kv heads, 50 MB: 10.4 us, of 18000 int8 rows, 28 MB: 8.1 us.)
 #include "rows.h"
 
 namespace psv {
 
 constexpr int kRowThreads = 256;
-constexpr int kTurnTile = 8;         // most rows of a workgroup that rotates (9500 rows of 12 heads: 12.0 us, with 16 rows 13.3)
+constexpr int kTurnTile = 8;         // most rows of a workgroup that rotates (9500 rows of 8 query and 2 kv heads: 12.0 us, with 16 rows 13.3)
 constexpr int kColumnTile = 32;      // most rows of a workgroup that transposes values; and up to 7 more, of its last octet
 constexpr int kColumnRows = kColumnTile + 7;
 
@@ -73,15 +75,32 @@ struct AppendArgs {
     uint32_t heads;                              // of a row in a rotating workgroup: queries, keys and, where they are rows, values
 };
 
-__device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float d, float scale)
-{
-    return quant_i8(a, scale) | (uint32_t)quant_i8(b, scale) << 8 | (uint32_t)quant_i8(c, scale) << 16 | (uint32_t)quant_i8(d, scale) << 24;
-}
+// Codes of N values of a row, clamp(rint(v / scale), -127, 127).  A correctly rounded division is some ten instructions; the product with 1 / scale
+// is within 127 * 2^-22 of it, so that both round to the same code unless the product is that near the middle between two: then, and for
+// scales whose reciprocal overflows, the division decides.  (Appending 8192 rows of 8 query and 8 kv heads: 21.3 us, with divisions 23.8.)
 template <int N>
 __device__ __forceinline__ void store_codes(uint8_t *p, const float (&v)[N], float scale)
 {
+    const float kMagic = 12582912.0f, r = 1.0f / scale;      // 1.5 * 2^23: adding it rounds to an integer (ties to even), which its low byte holds
+    uint32_t w[N / 4];
+    float far = 0.f;
 #pragma unroll
-    for (int e = 0; e < N; e += 4) reinterpret_cast<uint32_t *>(p)[e / 4] = pack_codes(v[e], v[e + 1], v[e + 2], v[e + 3], scale);
+    for (int e = 0; e < N; e += 4) {
+        float m[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            m[k] = fmaf(v[e + k], r, kMagic);
+            far = fmaxf(far, fabsf(fmaf(v[e + k], r, -(m[k] - kMagic))));
+        }
+        w[e / 4] = pack_magic_bytes(m[0], m[1], m[2], m[3]);
+    }
+    if (!(far < 0.4999f) || !(scale > 1e-30f)) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+            w[e / 4] = quant_i8(v[e], scale) | (uint32_t)quant_i8(v[e + 1], scale) << 8 | (uint32_t)quant_i8(v[e + 2], scale) << 16 | (uint32_t)quant_i8(v[e + 3], scale) << 24;
+    }
+#pragma unroll
+    for (int e = 0; e < N / 4; ++e) reinterpret_cast<uint32_t *>(p)[e] = w[e];
 }
 
 // Queries, keys and row-stored values: a head is shared by 128 / 2N lanes; a lane has two vectors of N channels: of rotated halves the two
@@ -277,11 +296,14 @@ hipError_t launch_cache_append(const psv_append_args &a, const psv_cache &cache,
     g.c = cache;
     if (rope) g.rope = *rope;
     const bool columns = cache.kv_layout == PSV_KV_HEAD_MAJOR;
-    g.turn_tile = tile_of(a.rows, kTurnTile);
+    g.heads = a.n_q_heads + cache.n_kv_heads * (columns ? 1 : 2);
+    // three heads a lane (2 / 3 / 4: 9500 rows of 10 heads 12.8 / 11.5 / 11.5 us, 16384 of 18 34.1 / 35.3 / 37.3, 16384 of 24 in 32 bits 63.7 /
+    // 65.2 / 65.4; with twelve 71.4)
+    const uint32_t most = 3 * (a.dtype == PSV_F32 ? kRowThreads / 16 : kRowThreads / 8) / g.heads;
+    g.turn_tile = tile_of(a.rows, most < 1 ? 1 : most < (uint32_t)kTurnTile ? most : kTurnTile);
     g.turn_groups = (a.rows + g.turn_tile - 1) / g.turn_tile;
     g.column_tile = tile_of(a.rows * cache.n_kv_heads, kColumnTile);
     g.column_groups = columns ? (a.rows + g.column_tile - 1) / g.column_tile : 0;
-    g.heads = a.n_q_heads + cache.n_kv_heads * (columns ? 1 : 2);
     const bool half = !rope || rope->pairing == PSV_ROPE_HALF;
     if (a.dtype == PSV_F32) half ? launch_append_as<PSV_F32, true>(g, s) : launch_append_as<PSV_F32, false>(g, s);
     else if (a.dtype == PSV_BF16) half ? launch_append_as<PSV_BF16, true>(g, s) : launch_append_as<PSV_BF16, false>(g, s);
@@ -432,7 +454,9 @@ static void launch_gather_as(const GatherArgs &g, hipStream_t s)
 hipError_t launch_cache_gather(const psv_gather_args &a, const psv_cache &cache, hipStream_t s)
 {
     const bool columns = cache.kv_layout == PSV_KV_HEAD_MAJOR;
-    GatherArgs g{a, cache, tile_of(a.rows, 32), 0, tile_of(a.rows * cache.n_kv_heads, kColumnTile), 0};
+    // four heads a lane of what lies as rows (16384 rows of 8 kv heads, token-major: 28.7 us, with 32 heads a lane 39.5)
+    const uint32_t most = 4 * (kRowThreads / 16) / (cache.n_kv_heads * (columns ? 1 : 2));
+    GatherArgs g{a, cache, tile_of(a.rows, most < 1 ? 1 : most < (uint32_t)kColumnTile ? most : kColumnTile), 0, tile_of(a.rows * cache.n_kv_heads, kColumnTile), 0};
     g.row_groups = (a.rows + g.row_tile - 1) / g.row_tile;
     g.column_groups = columns ? (a.rows + g.column_tile - 1) / g.column_tile : 0;
     if (a.dtype == PSV_F32) launch_gather_as<PSV_F32>(g, s);

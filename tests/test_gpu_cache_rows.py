@@ -301,6 +301,38 @@ def test_append_int8_rows_of_zeros_and_of_one_size():
     assert (vc[0] == 0).all() and vs[0] == 1.0 and (vc[1] == -127).all() and vc[2, 0, 0] == -127 and vc[2, 0, 127] == 127
 
 
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_append_int8_codes_are_the_rule_in_single_precision(dtype):
+    """Without rotation nothing but the rule is computed: scale = max|v| / 127 and code = rint(v / scale), bit for bit; among the values many
+    that lie on, or one rounding beside, the middle between two codes, and rows whose scale is tiny or has an infinite reciprocal."""
+    gen = torch.Generator().manual_seed(8)
+    n, nkv = 48, 2
+    v = torch.randn(n, nkv, 128, generator=gen)
+    half = torch.randint(-126, 126, (n, nkv, 128), generator=gen) + 0.5
+    near = half * (1.0 + torch.randint(-2, 3, half.shape, generator=gen) * 2.0 ** -23)
+    v[8:24] = near[8:24] * torch.rand(16, nkv, 1, generator=gen)
+    v[8:24, :, 0] = 127.0 * v[8:24, :, 0].sign()
+    v[24:32] = near[24:32]
+    v[24:32, :, 5] = -127.0
+    v[32] *= 1e-30
+    v[33] *= 1e-38
+    v[34] *= 1e-41
+    v[35] *= 1e30
+    v = v.to(TYPES[dtype])
+    k = v.flip(0).contiguous()
+    pools = Pools(4, nkv, "int8", "head", 8)
+    slots = dev(np.arange(5, 5 + n), torch.int64)
+    psv.psv_cache_append(None, k.cuda(), v.cuda(), None, None, slots, pools.cache, None, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for rows, (codes, scales) in zip((k, v), pools.rows(pools.gpu, slots.cpu())):
+        x = rows.float()
+        most = x.abs().amax(-1)
+        want = torch.where(most > 0, most / 127.0, torch.ones_like(most))
+        assert torch.equal(scales, want)
+        fine = (want > 0) & torch.isfinite(want)      # 1e30 is infinite in f16: inf / inf is no number, and has no code
+        assert torch.equal(codes[fine], torch.round(x / want[..., None]).clamp(-127, 127).double()[fine])
+
+
 @pytest.mark.parametrize("kv,layout", LAYOUTS)
 @pytest.mark.parametrize("dtype", sorted(TYPES))
 def test_gather_returns_what_is_cached(kv, layout, dtype):
