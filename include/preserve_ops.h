@@ -179,7 +179,8 @@ psv_status psv_cache_gather(const psv_gather_args *a, const psv_cache *cache, vo
  *
  * Tensor parallel: a shard has `columns` of the vocabulary, from `first_token` on.  psv_logprobs_part reduces them to `records` records
  * a row; the records of all shards, gathered behind one another, go to psv_logprobs_join, which gives every rank the answer.  psv_logprobs is
- * both, for one shard that has the whole vocabulary (columns = vocab, first_token = 0).  All shards take the same records, rows, given, top. */
+ * both, for one shard that has the whole vocabulary (columns = vocab, first_token = 0).  All shards take the same records, rows, given,
+ * top and scale. */
 #define PSV_LOGPROBS_MAX_TOP 32u
 #define PSV_LOGPROBS_MAX_GIVEN 32u
 #define PSV_LOGPROBS_MAX_RECORDS 256u      /* of all shards together, a row */

@@ -108,6 +108,19 @@ def test_slots_of_mixed_lengths(batch, longest, most, contiguous):
     check_slots(lens, new, contiguous=contiguous, n_free=batch * (most // 16 + 2), n_rows=int(new.sum()) + 77, seed=batch)      # padded
 
 
+@pytest.mark.parametrize("contiguous", [False, True])
+@pytest.mark.parametrize("batch", [120, 700, 2500])
+def test_slots_of_many_rows(batch, contiguous):
+    """More rows than compute units times threads, for each number of requests a lane: four rows a lane, and a last few behind them."""
+    rng = np.random.default_rng(batch)
+    most = 2 * 70000 // batch
+    lens, new = rng.integers(0, 640 - min(most, 600), size=batch), rng.integers(0, min(most, 600) + 1, size=batch)
+    new[rng.integers(0, batch, size=batch // 9)] = 0
+    n = max(int(new.sum()), 1 << 16) + 3
+    check_slots(lens, new, contiguous=contiguous, n_free=int((new // 16 + 2).sum()), n_rows=n, seed=batch)
+    check_slots(lens, new, contiguous=contiguous, n_free=int((new // 16 + 2).sum()) // 3, n_rows=n - 1000, seed=batch)      # some refused
+
+
 def test_slots_at_block_edges_and_without_rows():
     check_slots([0, 15, 16, 17, 31, 32, 0, 16], [16, 1, 16, 15, 1, 0, 0, 1])
     check_slots([0, 0, 0], [0, 0, 0], n_rows=0)
@@ -287,6 +300,21 @@ def test_append_without_rotation_skipped_and_scattered_rows(kv, layout):
     assert all(torch.equal(a.cpu(), b) for a, b in zip(pools.gpu, pools.before))
     append_case(100, 2, 3, kv, layout, scattered=True, blocks=30)
     append_case(70, 1, 1, kv, layout, scattered=True, blocks=70, dtype="f32", pairing="interleaved")
+
+
+@pytest.mark.parametrize("kv,layout", LAYOUTS)
+@pytest.mark.parametrize("n,nq,nkv,dtype,start", [(9001, 1, 1, "bf16", 3), (4099, 3, 3, "f32", 21), (2500, 0, 4, "f16", 0)])
+def test_append_and_gather_of_whole_tiles(n, nq, nkv, dtype, start, kv, layout):
+    """Rows enough for the largest tiles of both kinds of workgroups, some of them skipped, so that octets end inside tiles and across them."""
+    rng = np.random.default_rng(n)
+    skip = [(int(i), -1) for i in rng.integers(0, n, size=n // 40)]
+    pools, slots, (q, k, v) = append_case(n, nq, nkv, kv, layout, dtype, start=start, skip=skip)
+    out = torch.full((2, n, nkv, 128), 5.0, device="cuda")
+    psv.psv_cache_gather(dev(slots, torch.int64), out[0], out[1], pools.cache, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    ok = torch.as_tensor(slots >= 0)
+    for got, (value, scale) in zip(out, pools.rows(pools.gpu, slots[slots >= 0])):
+        assert torch.equal(got.cpu()[ok], value.float() if scale is None else value.float() * scale[..., None]) and (got.cpu()[~ok] == 5.0).all()
 
 
 def test_append_int8_rows_of_zeros_and_of_one_size():
