@@ -16,7 +16,7 @@
 namespace psv {
 
 constexpr int kThreads = kLogprobThreads, kWaves = kThreads / 64;
-constexpr uint32_t kList = PSV_LOGPROBS_MAX_TOP * 64;
+constexpr uint32_t kJoinList = PSV_LOGPROBS_MAX_TOP * 64;
 
 // Order of floats as unsigned integers (-0 counts as 0, every NaN is above infinity)
 __device__ __forceinline__ uint32_t order_of(float x)
@@ -147,10 +147,11 @@ struct Held {
 };
 
 template <uint32_t DT, int E>
-__global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 64 ? 4 : 6) : (E == 64 ? 6 : 8)) void k_logprobs_part(PartArgs g)
+__global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E == 64 ? 4 : 6) : (E == 128 ? 4 : E == 64 ? 6 : 8)) void k_logprobs_part(PartArgs g)
 {
     using T = typename Elem<DT>::T;
     constexpr int N = Elem<DT>::N, G = 8;
+    constexpr uint32_t kList = PSV_LOGPROBS_MAX_TOP * E;
     struct __attribute__((packed, aligned(sizeof(T)))) Loose { uint32_t w[4]; };      // rows of any alignment
     __shared__ Shared<kThreads, kList> sh;
     const psv_logprobs_args &a = g.a;
@@ -294,7 +295,8 @@ static void launch_part_as(const PartArgs &g, hipStream_t s)
     if (g.chunk <= kLogprobThreads * 8) PSV_LAUNCH((k_logprobs_part<DT, 8>), grid, block, 0, s, g);
     else if (g.chunk <= kLogprobThreads * 16) PSV_LAUNCH((k_logprobs_part<DT, 16>), grid, block, 0, s, g);
     else if (g.chunk <= kLogprobThreads * 32) PSV_LAUNCH((k_logprobs_part<DT, 32>), grid, block, 0, s, g);
-    else PSV_LAUNCH((k_logprobs_part<DT, 64>), grid, block, 0, s, g);
+    else if (g.chunk <= kLogprobThreads * 64) PSV_LAUNCH((k_logprobs_part<DT, 64>), grid, block, 0, s, g);
+    else PSV_LAUNCH((k_logprobs_part<DT, 128>), grid, block, 0, s, g);
 }
 
 hipError_t launch_logprobs_part(const psv_logprobs_args &a, float *records, hipStream_t s)
@@ -322,7 +324,7 @@ template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_logprobs_join(JoinArgs g)
 {
     constexpr int W = THREADS / 64;
-    constexpr uint32_t LIST = THREADS == 64 ? PSV_LOGPROBS_MAX_TOP * kHeld : kList;
+    constexpr uint32_t LIST = THREADS == 64 ? PSV_LOGPROBS_MAX_TOP * kHeld : kJoinList;
     __shared__ Shared<THREADS, LIST> sh;
     __shared__ float given_s[PSV_LOGPROBS_MAX_GIVEN];
     __shared__ uint32_t most_s[W];

@@ -209,7 +209,7 @@ uint32_t psv_logprobs_records(uint32_t rows, uint32_t columns)
     // The largest pieces, which cost least a column, that still give every compute unit one; below 4096 columns the records cost
     // more than the pieces gain.  (128256 columns in bf16, pieces of 16384 / 8192 / 4096 / 2048: 256 rows 28.1 / 33.5 / 45.5 / 69.8 us, 64
     // rows 17.2 / 18.3 / 22.0 / 29.6, 8 rows 13.7 / 12.8 / 12.8 / 16.1; 61 rows of 32003 13.4 / 12.2 / 11.8 / 13.4.)
-    uint32_t most = kLogprobMostColumns;
+    uint32_t most = kLogprobThreads * 64;
     while (most > 4096 && (uint64_t)rows * ((columns + most - 1) / most) < 256 && (columns + most / 2 - 1) / (most / 2) <= PSV_LOGPROBS_MAX_RECORDS) most /= 2;
     return (columns + most - 1) / most;
 }
@@ -240,6 +240,11 @@ psv_status psv_logprobs(const psv_logprobs_args *a, const psv_logprobs_out *out,
 {
     psv_logprobs_args b;
     ST_TRY(part_args(a, workspace, &b));
+    // Pieces of twice the size, where there are thousands, two columns fit a register and alternatives are wanted: what a piece costs beside its
+    // columns is halved (2048 rows of 128256 in bf16, none / 8 / 20 alternatives: 101.4 / 108.8 / 111.7 us against 97.5 / 112.8 / 120.1; 256
+    // rows 18.5 / 22.4 / 23.5 against 16.7 / 21.2 / 22.9).  These are fewer records than the workspace has room for.
+    const uint32_t fewer = (b.columns + kLogprobMostColumns - 1) / kLogprobMostColumns;
+    if (a->records == 0 && b.dtype != PSV_F32 && b.top >= 8 && fewer < b.records && (uint64_t)b.rows * fewer >= 2048) b.records = fewer;
     if (b.first_token != 0 || b.columns != b.vocab || workspace_bytes < psv_logprobs_bytes(b.rows, b.records, b.given, b.top)) return PSV_ERR_INVALID_ARG;
     if (!join_ok(&b, workspace, 1, out)) return PSV_ERR_INVALID_ARG;
     if (b.rows == 0) return PSV_OK;

@@ -195,6 +195,27 @@ def test_a_lane_that_holds_all_the_largest():
             check(x, given(8, 16384, 1), top=32, shards=[16384], records=1)
 
 
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_the_largest_pieces(dtype):
+    """128 columns a lane: by the rule (thousands of pieces), and by asking for one record; ties, lanes that hold all the largest, few left."""
+    n, v = 2100, 17003
+    x = logits(n, v, dtype, seed=9)
+    x[0], x[1, :] = 0.0, -INF
+    x[1, v - 1] = 1.0
+    x[2, ::7] = 30.0
+    t = given(n, v, 1, 9)
+    check(x, t, top=20)
+    y = logits(6, 32768, dtype, seed=10, size=0.5)
+    y[0], y[1, 5:], y[2, 100] = -2.0, -INF, NAN
+    vec = 4 if dtype == "f32" else 8
+    cols = (torch.arange(128 // vec)[:, None] * 256 * vec + torch.arange(vec)[None]).reshape(-1)
+    for lane in range(32):
+        y[3:, (cols + lane * vec).cuda()] = (20.0 + torch.arange(128.0) / 8).to(y.dtype).cuda()
+    for top in (1, 32):
+        check(y, given(6, 32768, 2), top=top, shards=[32768], records=1)
+        check(y[:, :30001], given(6, 30001, 2), top=top, shards=[30001], records=1)
+
+
 def test_ascending_and_far_offset_logits():
     v = 30000
     x = torch.stack([torch.linspace(-20, 20, v), torch.linspace(20, -20, v), 1.0e4 + 3 * torch.randn(v, generator=torch.Generator().manual_seed(2)),

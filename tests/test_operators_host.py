@@ -213,7 +213,7 @@ SHARED = [dict(tokens=None), dict(tokens=2 * P + 1), dict(rows=(1 << 20) + 1), d
 
 @pytest.mark.parametrize("kw", SHARED + [dict(logits=None), dict(logits=P + 2), dict(columns=0), dict(columns=(1 << 21) + 1), dict(first_token=1), dict(vocab=999),
                                          dict(first_token=0xffffffff), dict(dtype=3), dict(row=1 << 33), dict(row=-1000), dict(records=257),
-                                         dict(columns=128256, vocab=128256, row=128256, records=7)])
+                                         dict(columns=128256, vocab=128256, row=128256, records=3)])
 def test_logprobs_part_refuses(kw):
     L, a = psv.lib(), logprob_args(**kw)
     assert L.psv_logprobs_part(C.byref(a), 3 * P, None) == BAD
