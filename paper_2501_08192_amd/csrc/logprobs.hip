@@ -4,8 +4,10 @@
 // s (sum e d) / (sum e).  A workgroup reduces a piece of a row, its record, to (M, sum e, sum e d), the given tokens' logits and its largest
 // `top`; records are joined by rescaling their sums to the common M.  All sums are 32 bits; e d <= 0, so that nothing cancels.
 //
-// Bound by memory: a piece is read once, into registers, all loads at once, and everything else -- the maximum, the sums, the
-// alternatives -- is made from there.
+// A piece is read once, into registers, all loads at once, and everything else -- the maximum, the sums, the alternatives -- is made from
+// there.  Large calls in 32 bits are bound by memory (1024 rows of 128256, 525 MB: 92 us, 5.7 TB/s), in 16 bits by instructions: 13.5 a column,
+// a fourth of their time the exponential, which keep the vector units busy 99 % of the time (2048 rows, the same bytes: 109 us).  Small ones are bound by the
+// chain load -> bound -> candidates -> ranks, 5 us, and the same in the join.
 //
 // Alternatives without sorting: the top-th largest of the lanes' maxima is a bound T that at least `top` logits reach, and of every lane
 // but `top` none exceeds it; so at most top * (columns a lane) logits exceed T, usually about `top`.  Those that reach it are collected in LDS and
@@ -159,27 +161,34 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
     const uint32_t c0 = min(rec * g.chunk, a.columns), c1 = min(c0 + g.chunk, a.columns);
     const T *px = static_cast<const T *>(a.logits) + (int64_t)row * a.row;
     float *out = g.records + (size_t)blockIdx.x * record_floats(a.given, a.top);
-    Held<DT, E> x;
-#pragma unroll
-    for (int j = 0; j < E / N; ++j) {
+    // the lane's vector j of the piece; masked past its end
+    auto fetch = [&](uint32_t j, uint32_t (&w)[4]) {
         const uint32_t c = c0 + (j * kLogprobThreads + threadIdx.x) * N;
         if (c + N <= c1) {
             const Loose p = *reinterpret_cast<const Loose *>(px + c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x.w[j * 4 + i] = p.w[i];
-        } else {                                     // past the end of the piece: masked
+            for (int i = 0; i < 4; ++i) w[i] = p.w[i];
+        } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if constexpr (DT == PSV_F32) {
-                    x.w[j * 4 + i] = c + i < c1 ? __float_as_uint(px[c + i]) : 0xff800000u;
+                    w[i] = c + i < c1 ? __float_as_uint(px[c + i]) : 0xff800000u;
                 } else {
                     const uint16_t *ph = reinterpret_cast<const uint16_t *>(px);
                     const uint32_t none = DT == PSV_BF16 ? 0xff80u : 0xfc00u;
                     const uint32_t lo = c + 2 * i < c1 ? ph[c + 2 * i] : none, hi = c + 2 * i + 1 < c1 ? ph[c + 2 * i + 1] : none;
-                    x.w[j * 4 + i] = lo | hi << 16;
+                    w[i] = lo | hi << 16;
                 }
             }
         }
+    };
+    Held<DT, E> x;
+#pragma unroll
+    for (int j = 0; j < E / N; ++j) {
+        uint32_t w[4];
+        fetch(j, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.w[j * 4 + i] = w[i];
     }
     if (threadIdx.x < a.given) {
         const int64_t t = (int64_t)a.tokens[(size_t)row * a.given + threadIdx.x] - a.first_token;
@@ -230,11 +239,28 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
 #pragma unroll
         for (int i = 0; i < E / G; ++i) groups |= most[i] >= least ? 1u << i : 0u;
         auto id_of = [&](uint32_t i, uint32_t e) { return c0 + threadIdx.x * N + i * (G * kThreads) + e / N * (kThreads * N) + e % N; };
-        x.forget();
+        // Taken from the registers, a group costs a selection a word and group: large pieces, which are bound by their instructions, read it
+        // again instead (2048 rows of 32000 in bf16, 20 alternatives: 38.0 us against 40.2); small ones would wait for the trip.
+        auto group = [&](uint32_t i) {
+            if constexpr (E < 64) {
+                return x.group(i);
+            } else {
+                Held<DT, G> h;
+#pragma unroll
+                for (int j = 0; j < G / N; ++j) {
+                    uint32_t w[4];
+                    fetch(i * (G / N) + j, w);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) h.w[j * 4 + k] = w[k];
+                }
+                return h;
+            }
+        };
+        if (E < 64) x.forget();
         for (int pass = 0;; ++pass) {
             for (uint32_t left = groups; left; left &= left - 1) {
                 const uint32_t i = __builtin_ctz(left);
-                const Held<DT, G> h = x.group(i);
+                const Held<DT, G> h = group(i);
                 uint32_t hits = 0;
 #pragma unroll
                 for (int e = G - 1; e >= 0; --e) hits = 2 * hits + (h.get(e) >= least);
@@ -257,7 +283,7 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
                 key = ~0u;
             } else if (groups) {
                 const uint32_t i = __builtin_ctz(groups);
-                const Held<DT, G> h = x.group(i);
+                const Held<DT, G> h = group(i);
 #pragma unroll
                 for (int e = G - 1; e >= 0; --e)
                     if (h.get(e) == least) key = ~id_of(i, e);
