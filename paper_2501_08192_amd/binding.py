@@ -440,12 +440,16 @@ def _type(t):
 
 
 _ROW_TYPES = {"float32": PSV_F32, "bfloat16": PSV_BF16, "float16": PSV_F16}
+_ROW_CODES = {}  # ... -> its code as rows' element type
 
 
 def _dtype(name, t):
-    code = _ROW_TYPES.get(_type(t))
+    code = _ROW_CODES.get(t.dtype)
     if code is None:
-        raise ValueError("%s: float32, bfloat16 or float16 is wanted, got %s" % (name, t.dtype))
+        code = _ROW_TYPES.get(_type(t))
+        if code is None:
+            raise ValueError("%s: float32, bfloat16 or float16 is wanted, got %s" % (name, t.dtype))
+        _ROW_CODES[t.dtype] = code
     return code
 
 
@@ -459,7 +463,7 @@ def _rows(name, t):
 
 def _want(name, t, dtype, *shape):
     """The address of a contiguous tensor of a type and shape."""
-    if _type(t) != dtype or t.shape != shape or not t.is_contiguous():
+    if (_TYPES.get(t.dtype) or _type(t)) != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: contiguous %s %s is wanted, got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
     return t.data_ptr()
 
