@@ -5,9 +5,9 @@
 // `top`; records are joined by rescaling their sums to the common M.  All sums are 32 bits; e d <= 0, so that nothing cancels.
 //
 // A piece is read once, into registers, all loads at once, and everything else -- the maximum, the sums, the alternatives -- is made from
-// there.  Large calls in 32 bits are bound by memory (1024 rows of 128256, 525 MB: 92 us, 5.7 TB/s), in 16 bits by instructions: 13.5 a column,
-// a fourth of their time the exponential, which keep the vector units busy 99 % of the time (2048 rows, the same bytes: 109 us).  Small ones are bound by the
-// chain load -> bound -> candidates -> ranks, 5 us, and the same in the join.
+// there.  Large calls in 32 bits are bound by memory (1024 rows of 128256, 525 MB: 92 us, 5.7 TB/s), in 16 bits by instructions, 11.4 a column of
+// which the exponential takes the time of four (2048 rows, the same bytes: 101 us, the vector units busy 91 % of it).  Small ones are bound by
+// the chain load -> bound -> candidates -> ranks, 5 us, and the same in the join.
 //
 // Alternatives without sorting: the top-th largest of the lanes' maxima is a bound T that at least `top` logits reach, and of every lane
 // but `top` none exceeds it; so at most top * (columns a lane) logits exceed T, usually about `top`.  Those that reach it are collected in LDS and
@@ -216,13 +216,18 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
     top_order = wave_max_u32(top_order);
     const bool bad = top_order >= kOrderInf;          // a NaN or +infinity
     const float M = of_order(top_order), ref = top_order == kOrderNone ? 0.f : M;
+    // In units of log 2, t = x c - M c as one multiply-add: M c is rounded, which moves every t by the same `shift`, known exactly and taken out of
+    // the sums at their end.  (With the difference first a column costs an instruction more: 2048 rows of 128256 in bf16 108.8 us against 100.6.)  From
+    // 2^90 on M c may overflow, but there logits that differ do so by 2^66 at least: with c = 1 all but the largest vanish as they would.
+    const bool huge = fabsf(ref) >= 0x1p90f;
+    const float c = huge ? 1.f : g.to_log2, Mc = ref * c, shift = fmaf(ref, c, -Mc);
     float s = 0.f, w = 0.f;
     x.forget();
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float d = fmaxf(x.get(e) - ref, kLowest), p = exp2_raw(d * g.to_log2);      // a masked logit: p = 0 and a finite d
+        const float t = fmaxf(fmaf(x.get(e), c, -Mc), kLowest), p = exp2_raw(t);      // a masked logit: p = 0 and a finite t
         s += p;
-        w = fmaf(p, d, w);
+        w = fmaf(p, t, w);
     }
     s = wave_sum(s);
     w = wave_sum(w);
@@ -307,9 +312,10 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
     }
     if (threadIdx.x == 0) {
         const float2 a0 = sh.sums[0], a1 = sh.sums[1], a2 = sh.sums[2], a3 = sh.sums[3];
+        const float S = (a0.x + a1.x) + (a2.x + a3.x), D = (a0.y + a1.y) + (a2.y + a3.y), back = exp2_raw(-shift);
         out[0] = M;
-        out[1] = bad ? nan32() : (a0.x + a1.x) + (a2.x + a3.x);
-        out[2] = (a0.y + a1.y) + (a2.y + a3.y);
+        out[1] = bad ? nan32() : S * back;
+        out[2] = fmaf(-shift, S, D) * back / c;         // of d = t / c
         out[3] = 0.f;
     }
 }

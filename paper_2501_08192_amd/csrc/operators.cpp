@@ -241,8 +241,8 @@ psv_status psv_logprobs(const psv_logprobs_args *a, const psv_logprobs_out *out,
     psv_logprobs_args b;
     ST_TRY(part_args(a, workspace, &b));
     // Pieces of twice the size, where there are thousands, two columns fit a register and alternatives are wanted: what a piece costs beside its
-    // columns is halved (2048 rows of 128256 in bf16, none / 8 / 20 alternatives: 101.4 / 108.8 / 111.7 us against 97.5 / 112.8 / 120.1; 256
-    // rows 18.5 / 22.4 / 23.5 against 16.7 / 21.2 / 22.9).  These are fewer records than the workspace has room for.
+    // columns is halved (2048 rows of 128256 in bf16, none / 8 / 20 alternatives: 97.3 / 100.6 / 107.5 us against 93.6 / 102.0 / 111.1; 256
+    // rows 17.9 / 21.1 / 21.9 against 16.6 / 20.4 / 22.0).  These are fewer records than the workspace has room for.
     const uint32_t fewer = (b.columns + kLogprobMostColumns - 1) / kLogprobMostColumns;
     if (a->records == 0 && b.dtype != PSV_F32 && b.top >= 8 && fewer < b.records && (uint64_t)b.rows * fewer >= 2048) b.records = fewer;
     if (b.first_token != 0 || b.columns != b.vocab || workspace_bytes < psv_logprobs_bytes(b.rows, b.records, b.given, b.top)) return PSV_ERR_INVALID_ARG;
