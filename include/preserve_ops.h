@@ -116,7 +116,7 @@ typedef struct {
     int32_t *seq_lens;            /* dev [batch] out: lens + new_lens, or lens where refused: psv_kv_desc's seq_lens of a decode step */
     int32_t *row_starts;          /* dev [batch + 1] out: first row of each request and the end of the last, at most `rows` */
     int64_t *slots;               /* dev [rows] out; -1 for rows of refused requests and behind the last */
-    int32_t *positions;           /* dev [rows] out; 0 behind the last row */
+    int32_t *positions;           /* dev [rows] out: lens + place within the request, refused ones included; 0 behind the last row */
     int32_t *requests;            /* dev [rows] out: the row's request; -1 behind the last row */
     int32_t *free_range_out;      /* dev [2] out; NULL without a block table */
     int32_t *refused;             /* dev [1] out: how many requests were refused */

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kSlotsThreads) void k_cache_slots(psv_slots_args a)
         taken = add_sat(taken, need);
         if (table && need && taken > (uint32_t)free_n) good = false;
         start_s[b] = (int32_t)min(row, a.rows);
-        first_s[b] = good ? (table ? head + (int32_t)before : 0) : -1;
+        first_s[b] = !good ? -1 : table && need ? head + (int32_t)before : 0;
         refused += !good;
         if (good && need) used = taken;                           // those that are not refused come first: the last one's end is their sum
         row = add_sat(row, (uint32_t)max(n, (int64_t)0));

@@ -193,3 +193,31 @@ def test_set_rope_on_a_context_without_rotation():
         assert not torch.equal(s.run(), plain)
         psv.psv_set_rope(s.ctx, None)
         assert torch.equal(s.run(), plain)
+
+
+@pytest.mark.parametrize("fused", [0, 1, 2])
+def test_every_kind_of_step_rotates_with_them(fused):
+    """Kernels of an operator, of a block, of the whole step: the same output and keys to rounding."""
+    w = synth.Workload("rope_fused", 2, 4096, 4, 1, 128, 1792, 1, 300, False, (0.0, 0.0))
+    rope = psv.psv_rope_plan(theta=w.rope_theta, scaling="turns", factor=8.0, trained_context=100.0, magnitude=1.1)
+    got = {}
+    for kind in {0, fused}:
+        with Session(w, seed=13, fused=kind) as s:
+            psv.psv_set_rope(s.ctx, rope)
+            got[kind] = (s.run().clone().cpu(), s.k_pools[0].cpu().float())
+            assert psv.psv_debug_last_step_path(s.ctx) == kind
+    (a, ka), (b, kb) = got[fused], got[0]
+    assert ((a - b).abs() <= 2e-2 + 1e-2 * b.abs()).all()
+    assert ((ka - kb).abs() <= kb.abs() * 2.0 ** -7).all()      # a key on either side of a rounding: one step
+
+
+@pytest.mark.parametrize("batch", [1, 8])
+def test_the_policies_agree_bit_for_bit_with_frequencies_set(batch):
+    w = synth.Workload("rope_windows", 3, 4096, 4, 1, 128, 1792, batch, 200, True, (15.0, 15.0))
+    from paper_2501_08192_amd.harness import default_policy
+    with Session(w, seed=14) as s:
+        psv.psv_set_rope(s.ctx, psv.psv_rope_plan(theta=w.rope_theta, scaling="linear", factor=4.0))
+        off = s.run().clone()
+        for kw in (dict(), dict(prelaunch=0)):
+            s.set_policy(default_policy(w, **kw))
+            assert torch.equal(s.run(), off)
