@@ -69,7 +69,8 @@ __device__ __forceinline__ int nth_bit(uint64_t x, uint32_t n)
 struct AppendArgs {
     psv_append_args a;
     psv_cache c;
-    psv_rope rope;                   // dims 0: not rotated
+    uint32_t dims;                   // rotated channels; 0: not rotated
+    double magnitude, freq[PSV_HEAD_DIM / 2];
     uint32_t turn_tile, turn_groups;             // workgroups [0, turn_groups): rotate
     uint32_t column_tile, column_groups;         // the others: values by columns, column_groups of them a kv head
     uint32_t heads;                              // of a row in a rotating workgroup: queries, keys and, where they are rows, values
@@ -111,8 +112,8 @@ __device__ __forceinline__ void append_rows(const AppendArgs &g, float2 *cs, int
     using T = typename Elem<DT>::T;
     constexpr int N = Elem<DT>::N, LANES = 64 / N, HEADS = kRowThreads / LANES;
     const psv_append_args &a = g.a;
-    const uint32_t row0 = blockIdx.x * g.turn_tile, n_rows = min(g.turn_tile, a.rows - row0), n = g.rope.dims / 2;
-    const double m = g.rope.magnitude;
+    const uint32_t row0 = blockIdx.x * g.turn_tile, n_rows = min(g.turn_tile, a.rows - row0), n = g.dims / 2;
+    const double m = g.magnitude;
     const uint32_t lane = threadIdx.x % LANES, nq = a.n_q_heads, nkv = g.c.n_kv_heads, heads = g.heads;
     const bool turned = lane * 2 * N < 2 * n;
     const uint32_t lo = HALF && turned ? lane * N : lane * 2 * N, hi = HALF && turned ? n + lane * N : lo + N;
@@ -132,7 +133,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs &g, float2 *cs, int
     for (int i = threadIdx.x; i < (int)n_rows; i += kRowThreads) slots[i] = a.slots[row0 + i];
     for (uint32_t i = threadIdx.x; i < n_rows * 64; i += kRowThreads) {
         const uint32_t p = i & 63;
-        if (p < n) cs[i] = turn((double)a.positions[row0 + (i >> 6)] * g.rope.freq[p], m);
+        if (p < n) cs[i] = turn((double)a.positions[row0 + (i >> 6)] * g.freq[p], m);
     }
     __syncthreads();
     while (r < n_rows) {
@@ -294,7 +295,11 @@ hipError_t launch_cache_append(const psv_append_args &a, const psv_cache &cache,
     AppendArgs g{};
     g.a = a;
     g.c = cache;
-    if (rope) g.rope = *rope;
+    if (rope) {
+        g.dims = rope->dims;
+        g.magnitude = rope->magnitude;
+        for (uint32_t i = 0; i < rope->dims / 2; ++i) g.freq[i] = rope->freq[i];
+    }
     const bool columns = cache.kv_layout == PSV_KV_HEAD_MAJOR;
     g.heads = a.n_q_heads + cache.n_kv_heads * (columns ? 1 : 2);
     // three heads a lane (2 / 3 / 4: 9500 rows of 10 heads 12.8 / 11.5 / 11.5 us, 16384 of 18 34.1 / 35.3 / 37.3, 16384 of 24 in 32 bits 63.7 /
