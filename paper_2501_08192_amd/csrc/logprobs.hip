@@ -127,6 +127,25 @@ struct Held {
         else if constexpr (DT == PSV_BF16) return e & 1 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
         else return (float)__builtin_bit_cast(_Float16, (uint16_t)(e & 1 ? w[e / 2] >> 16 : w[e / 2]));
     }
+    // Column e, known only when it runs, of one group.  The empty asm keeps the selections in registers: without it the
+    // compiler may make the words an array in scratch.
+    __device__ float pick(uint32_t e) const
+    {
+        constexpr int W = kHalves ? E / 2 : E;
+        static_assert(E == 8, "one group");   // four or eight words: a chain of selections is short
+        const uint32_t k = kHalves ? e >> 1 : e;
+        uint32_t v = w[0];
+        asm volatile("" : "+v"(v));
+#pragma unroll
+        for (uint32_t j = 1; j < (uint32_t)W; ++j) {
+            v = k == j ? w[j] : v;
+            asm volatile("" : "+v"(v));
+        }
+        if constexpr (!kHalves) return __uint_as_float(v);
+        v = e & 1 ? v >> 16 : v & 0xffffu;
+        if constexpr (DT == PSV_BF16) return __uint_as_float(v << 16);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)v);
+    }
     // Columns 8 i to 8 i + 7
     __device__ Held<DT, 8> group(uint32_t i) const
     {
@@ -274,9 +293,11 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
                     for (int e = 0; e < G; ++e)
                         if (h.get(e) == least && id_of(i, e) > last) hits &= ~(1u << e);
                 uint32_t at = list_places(&sh.count, (uint32_t)__popc(hits));
-#pragma unroll
-                for (int e = 0; e < G; ++e)
-                    if ((hits >> e & 1) && at < kList) sh.list[at++] = list_entry(order_of(h.get(e)), id_of(i, e));
+                // A step a hit, mostly one, not a test a column (61 rows of 32003 for 20: 7.0 us against 7.4; 2048 of 128256: 114 against 117)
+                for (; hits && at < kList; hits &= hits - 1) {
+                    const uint32_t e = __builtin_ctz(hits);
+                    sh.list[at++] = list_entry(order_of(h.pick(e)), id_of(i, e));
+                }
             }
             __syncthreads();
             n = sh.count;
