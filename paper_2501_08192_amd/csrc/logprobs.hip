@@ -6,7 +6,7 @@
 //
 // A piece is read once, into registers, all loads at once, and everything else -- the maximum, the sums, the alternatives -- is made from
 // there.  Large calls in 32 bits are bound by memory (1024 rows of 128256, 525 MB: 92 us, 5.7 TB/s), in 16 bits by instructions, 11.4 a column of
-// which the exponential takes the time of four (2048 rows, the same bytes: 101 us, the vector units busy 91 % of it).  Small ones are bound by
+// which the exponential takes the time of four (2048 rows, the same bytes: 101 us, the vector units busy 92 % of it).  Small ones are bound by
 // the chain load -> bound -> candidates -> ranks, 5 us, and the same in the join.
 //
 // Alternatives without sorting: the top-th largest of the lanes' maxima is a bound T that at least `top` logits reach, and of every lane
