@@ -2,7 +2,8 @@
 //
 // With M the largest logit of a row, d = x - M (exact, or one rounding) and e = exp(s d):  ln p = s d - ln(sum e), entropy = ln(sum e) -
 // s (sum e d) / (sum e).  A workgroup reduces a piece of a row, its record, to (M, sum e, sum e d), the given tokens' logits and its largest
-// `top`; records are joined by rescaling their sums to the common M.  All sums are 32 bits; e d <= 0, so that nothing cancels.
+// `top`; records are joined by rescaling their sums to the common M.  All sums are 32 bits.  No term e d is positive, so that nothing cancels but the
+// common rounding of the exponents, at most a quarter of a unit (below).
 //
 // A piece is read once, into registers, all loads at once, and everything else -- the maximum, the sums, the alternatives -- is made from
 // there.  Large calls in 32 bits are bound by memory (1024 rows of 128256, 525 MB: 92 us, 5.7 TB/s), in 16 bits by instructions, 11.4 a column of
@@ -236,17 +237,31 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
     const bool bad = top_order >= kOrderInf;          // a NaN or +infinity
     const float M = of_order(top_order), ref = top_order == kOrderNone ? 0.f : M;
     // In units of log 2, t = x c - M c as one multiply-add: M c is rounded, which moves every t by the same `shift`, known exactly and taken out of
-    // the sums at their end.  (With the difference first a column costs an instruction more: 2048 rows of 128256 in bf16 108.8 us against 100.6.)  From
-    // 2^90 on M c may overflow, but there logits that differ do so by 2^66 at least: with c = 1 all but the largest vanish as they would.
-    const bool huge = fabsf(ref) >= 0x1p90f;
-    const float c = huge ? 1.f : g.to_log2, Mc = ref * c, shift = fmaf(ref, c, -Mc);
+    // the sums at their end.  (With the difference first a column costs an instruction more: 2048 rows of 128256 in bf16 108.8 us against 100.6.)
+    // Below 2^23 the rounding is at most 1/4, which scales the sums by 2^(1/4) at most and costs the second a quarter of the first's error.  From there
+    // on -- a large scale, or a piece of nothing but far values -- it would leave the exponential's range: the difference first, of columns read again.
+    const float c = g.to_log2;
+    const bool near = fabsf(ref * c) < 0x1p23f;
+    const float Mc = near ? ref * c : 0.f, shift = near ? fmaf(ref, c, -Mc) : 0.f;
     float s = 0.f, w = 0.f;
-    x.forget();
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const float t = fmaxf(fmaf(x.get(e), c, -Mc), kLowest), p = exp2_raw(t);      // a masked logit: p = 0 and a finite t
+    auto add = [&](float t) {
+        t = fmaxf(t, kLowest);          // a masked logit: p = 0 and a finite t
+        const float p = exp2_raw(t);
         s += p;
         w = fmaf(p, t, w);
+    };
+    x.forget();
+    if (near) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) add(fmaf(x.get(e), c, -Mc));
+    } else {
+#pragma unroll 1
+        for (int j = 0; j < E / N; ++j) {
+            Held<DT, N> h;
+            fetch(j, h.w);
+#pragma unroll
+            for (int e = 0; e < N; ++e) add((h.get(e) - ref) * c);
+        }
     }
     s = wave_sum(s);
     w = wave_sum(w);
