@@ -137,7 +137,8 @@ typedef struct {
 
 /* The rows of a prompt, or of one step of a program with its own attention: queries and keys are rotated (rope != NULL), keys and
  * values go into the cache, as the decode step does with its one token a sequence: computed in 32 bits, then rounded to bf16, or
- * quantised to int8 by the rule in preserve.h.  Rows are [heads][128] elements, rows of 16-byte aligned starts.
+ * quantised to int8 by the rule in preserve.h.  (A quotient that is not a number has the code -127 in both: a NaN's, and that of an infinity in its
+ * own row, whose scale is infinite and whose finite elements have code 0.)  Rows are [heads][128] elements, rows of 16-byte aligned starts.
  * A slot outside [0, num_pool_blocks * 16) skips the row's key and value (its query is still rotated).  Slots must differ: which of
  * the rows that share one it ends up with, channel by channel, is not defined.
  * rope->dims must be a multiple of 16 and at most 128 (PSV_ERR_UNSUPPORTED). */

@@ -77,8 +77,8 @@ struct AppendArgs {
 };
 
 // Codes of N values of a row, clamp(rint(v / scale), -127, 127).  A correctly rounded division is some ten instructions; the product with 1 / scale
-// is within 127 * 2^-22 of it, so that both round to the same code unless the product is that near the middle between two: then, and for
-// scales whose reciprocal overflows, the division decides.  (Appending 8192 rows of 8 query and 8 kv heads: 21.3 us, with divisions 23.8.)
+// is within 127 * 2^-22 of it, so that both round to the same code unless the product is that near the middle between two: then, for
+// scales whose reciprocal overflows, and where a product is no number (a NaN, an infinity times zero; the maximum hands it on), the division decides.  (Appending 8192 rows of 8 query and 8 kv heads: 21.3 us, with divisions 23.8.)
 template <int N>
 __device__ __forceinline__ void store_codes(uint8_t *p, const float (&v)[N], float scale)
 {
@@ -91,7 +91,7 @@ __device__ __forceinline__ void store_codes(uint8_t *p, const float (&v)[N], flo
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             m[k] = fmaf(v[e + k], r, kMagic);
-            far = fmaxf(far, fabsf(fmaf(v[e + k], r, -(m[k] - kMagic))));
+            far = __builtin_elementwise_maximum(far, fabsf(fmaf(v[e + k], r, -(m[k] - kMagic))));
         }
         w[e / 4] = pack_magic_bytes(m[0], m[1], m[2], m[3]);
     }
