@@ -44,11 +44,8 @@ psv_status psv_create(const psv_model_desc *desc, void *stream_main, void *strea
         return fail(PSV_ERR_NOMEM);
     }
     if (hipMemset(c->wsp, 0, c->ws.total) != hipSuccess) return fail(PSV_ERR_HIP);
-    if (c->d.rope_theta > 0.f) {
-        double f[64];
-        for (int i = 0; i < 64; ++i) f[i] = pow((double)c->d.rope_theta, -2.0 * (double)i / 128.0);
-        if (hipMemcpy(c->wsp + c->ws.inv_freq, f, sizeof f, hipMemcpyHostToDevice) != hipSuccess) return fail(PSV_ERR_HIP);
-    }
+    const StepRope r = step_rope(c->d.rope_theta);
+    if (hipMemcpy(c->wsp + c->ws.rope_freq, &r, sizeof r, hipMemcpyHostToDevice) != hipSuccess) return fail(PSV_ERR_HIP);
     c->weights.resize(c->d.n_layers);
     c->weights_set.assign(c->d.n_layers, 0);
     c->k_pools.assign(c->d.n_layers, nullptr);

@@ -69,8 +69,8 @@ __device__ __forceinline__ void make_attn_plan(const int32_t *seq_lens, int max_
 // is formed and reduced in double (position * theta^(-2i/128)), so long contexts lose nothing to
 // fp32 range reduction.  The position is the same for every layer, so this runs once per step -- as does the plan of the
 // attention's work, by one more workgroup (blockIdx.x == batch).
-__global__ __launch_bounds__(64) void k_rope_table(const int32_t *__restrict__ seq_lens, const double *__restrict__ inv_freq,
-                                                   double magnitude, int max_tokens, int batch, float2 *__restrict__ table, AttnPlan plan)
+__global__ __launch_bounds__(64) void k_rope_table(const int32_t *__restrict__ seq_lens, const StepRope *__restrict__ rope,
+                                                   int max_tokens, int batch, float2 *__restrict__ table, AttnPlan plan)
 {
     const int b = blockIdx.x, i = threadIdx.x;
     if (b == batch) {
@@ -79,33 +79,28 @@ __global__ __launch_bounds__(64) void k_rope_table(const int32_t *__restrict__ s
     }
     int T = seq_lens[b];
     if (T < 1 || T > max_tokens) T = 1;
-    float2 cs = make_float2(1.f, 0.f);
-    if (inv_freq) {
-        double sd, cd;
-        sincos((double)(T - 1) * inv_freq[i], &sd, &cd);
-        cs = make_float2((float)(cd * magnitude), (float)(sd * magnitude));
-    }
-    table[b * 64 + i] = cs;
+    double sd, cd;
+    sincos((double)(T - 1) * rope->freq[i], &sd, &cd);      // of 0: exactly 0 and 1
+    table[b * 64 + i] = make_float2((float)(cd * rope->magnitude), (float)(sd * rope->magnitude));
 }
 
-hipError_t launch_rope_table(const int32_t *seq_lens, const double *inv_freq, double magnitude, int max_tokens, int batch, float2 *table,
+hipError_t launch_rope_table(const int32_t *seq_lens, const StepRope *rope, int max_tokens, int batch, float2 *table,
                              const AttnPlan *plan, hipStream_t s)
 {
     if (plan && (batch > 64 || plan->slots < batch)) return hipErrorInvalidValue;
-    PSV_LAUNCH(k_rope_table, dim3(batch + (plan ? 1 : 0)), dim3(64), 0, s, seq_lens, inv_freq, magnitude, max_tokens, batch, table, plan ? *plan : AttnPlan{});
+    PSV_LAUNCH(k_rope_table, dim3(batch + (plan ? 1 : 0)), dim3(64), 0, s, seq_lens, rope, max_tokens, batch, table, plan ? *plan : AttnPlan{});
     return hipGetLastError();
 }
 
-struct FreqTable {
-    double f[64];
-};
-__global__ __launch_bounds__(64) void k_store_freq(FreqTable t, double *dst) { dst[threadIdx.x] = t.f[threadIdx.x]; }
-
-hipError_t launch_store_freq(const double *freq, double *dst, hipStream_t s)
+__global__ __launch_bounds__(64) void k_store_rope(StepRope r, StepRope *dst)
 {
-    FreqTable t;
-    for (int i = 0; i < 64; ++i) t.f[i] = freq[i];
-    PSV_LAUNCH(k_store_freq, dim3(1), dim3(64), 0, s, t, dst);
+    dst->freq[threadIdx.x] = r.freq[threadIdx.x];
+    if (threadIdx.x == 0) dst->magnitude = r.magnitude;
+}
+
+hipError_t launch_store_rope(const StepRope &rope, StepRope *dst, hipStream_t s)
+{
+    PSV_LAUNCH(k_store_rope, dim3(1), dim3(64), 0, s, rope, dst);
     return hipGetLastError();
 }
 

@@ -19,7 +19,7 @@ struct Workspace {
     size_t total = 0;
     // offsets
     size_t x, y, h1_f32, h1_bf16, h2_f32, h2_bf16, qkv, rope, part_ml, part_o, attn_f32, attn_bf16,
-        delta_a, delta_m, m_f32, m_bf16, inv_freq, flag, part, ssq, ssq_ll, m_ll, qkv_ll, pml_ll, po_ll, step_tbl, step_ll, seg_ind, seg_pml, seg_po, seg_m;
+        delta_a, delta_m, m_f32, m_bf16, rope_freq, flag, part, ssq, ssq_ll, m_ll, qkv_ll, pml_ll, po_ll, step_tbl, step_ll, seg_ind, seg_pml, seg_po, seg_m;
 };
 
 Workspace layout_workspace(const psv_model_desc &d);
@@ -60,8 +60,6 @@ struct psv_ctx {
     bool last_step_planned = false;              // the last step's attention was split by the lengths of the step
     int overlap = -1;                            // psv_check_overlap's last answer (-1 = not run yet)
     bool check_err_word = false;                 // a kernel that may set the error word (a pre-launched consumer, a fused kernel) was launched: read it at sync
-    bool rope_set = false;                       // psv_set_rope: the frequencies in the workspace are the caller's ...
-    double rope_magnitude = 1.0;                 // ... and so is the magnitude of the rotated channels
     int fused = 3;                               // psv_set_fused_kernels: 0 one kernel per operator, 1 one per block, 2 one per step, 3 by shape
     bool step_tbl_dirty = true;                  // the per-layer pointer table of the whole-step kernel has to be uploaded again
     std::vector<unsigned char> step_tbl_host;    // ... its host copy (kept alive until the upload has run)

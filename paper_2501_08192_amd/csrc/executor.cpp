@@ -16,6 +16,14 @@
 
 namespace psv {
 
+StepRope step_rope(float theta)
+{
+    StepRope r{};
+    r.magnitude = 1.0;
+    for (int i = 0; i < 64 && theta > 0.f; ++i) r.freq[i] = pow((double)theta, -2.0 * (double)i / 128.0);
+    return r;
+}
+
 Workspace layout_workspace(const psv_model_desc &d)
 {
     Workspace w;
@@ -48,7 +56,7 @@ Workspace layout_workspace(const psv_model_desc &d)
     w.delta_m = take(B * H * 4);
     w.m_f32 = take(B * F * 4);
     w.m_bf16 = take(2 * Bp * F * 2);
-    w.inv_freq = take(64 * sizeof(double));
+    w.rope_freq = take(sizeof(StepRope));
     w.flag = take(256);
     w.ssq = take(B * (H / 512) * 4);
     w.ssq_ll = take(kSkTagCopies * sk_tag_stride((int)B, (int)H) * 8);     // the same as tagged values (in copies), for a projection launched ahead of them
@@ -393,13 +401,12 @@ static psv_status enqueue_whole_step(psv_ctx *c, const float *x_in, float *x_out
     }
     const KvView kv = kv_view(c, lb, 1);
     float2 *rope = c->at<float2>(c->ws.rope);
-    const double *inv_freq = d.rope_theta > 0.f || c->rope_set ? c->at<double>(c->ws.inv_freq) : nullptr;
     c->last_prefetch_launches = 0;
     c->last_step_prelaunches = 0;
     c->step_launches = 0;
     c->step_layers = le - lb;
     ST_TRY(prof_tag(c, -2));
-    HIP_TRY(launch_rope_table(c->kv.seq_lens, inv_freq, c->rope_magnitude, kv.max_tokens, 1, rope, nullptr, s));
+    HIP_TRY(launch_rope_table(c->kv.seq_lens, c->at<StepRope>(c->ws.rope_freq), kv.max_tokens, 1, rope, nullptr, s));
     StepLaunch p{};
     p.layer_table = c->wsp + c->ws.step_tbl;
     p.lb = (int)lb; p.le = (int)le;
@@ -459,7 +466,6 @@ psv_status enqueue_step(psv_ctx *c, const float *x_in, float *x_out, uint32_t ba
     uint16_t *attnb = c->at<uint16_t>(c->ws.attn_bf16), *mb = c->at<uint16_t>(c->ws.m_bf16);
     float *pml = c->at<float>(c->ws.part_ml), *po = c->at<float>(c->ws.part_o);
     float2 *rope = c->at<float2>(c->ws.rope);
-    const double *inv_freq = d.rope_theta > 0.f || c->rope_set ? c->at<double>(c->ws.inv_freq) : nullptr;
     Lanes ln{c->main, c->side};
     hipStream_t &s = ln.cur;          // the stream the operator chain is on (changes at a pre-launching window)
     GemvWait wait{};
@@ -559,7 +565,7 @@ psv_status enqueue_step(psv_ctx *c, const float *x_in, float *x_out, uint32_t ba
     c->last_step_planned = plan != nullptr;
 
     ST_TRY(prof_tag(c, -2));
-    HIP_TRY(launch_rope_table(c->kv.seq_lens, inv_freq, c->rope_magnitude, kv_view(c, lb, batch).max_tokens, B, rope, made, s));
+    HIP_TRY(launch_rope_table(c->kv.seq_lens, c->at<StepRope>(c->ws.rope_freq), kv_view(c, lb, batch).max_tokens, B, rope, made, s));
     const float *res = x_in, *delta = nullptr;   // residual stream entering the layer = res + delta
     int delta_splits = 1;                        // delta may be a stack of split-K partials
     for (uint32_t l = lb; l < le; ++l) {

@@ -209,12 +209,20 @@ hipError_t launch_resid_sum(const float *res, const float *delta, int delta_spli
 // Gate | up: out = silu(gate) * up of the summed splits, width N/2, also as the next projection's operand in out_bf16.
 hipError_t launch_sk_reduce(const float *part, int splits, int batch, int N, float *out, uint16_t *out_bf16, bool digits, hipStream_t s);
 
-// cos/sin of the rotary angles at position seq_len-1, times magnitude: table [batch][64] (inv_freq null => identity); optionally
-// the step's plan.
-hipError_t launch_rope_table(const int32_t *seq_lens, const double *inv_freq, double magnitude, int max_tokens, int batch,
+// What a step rotates with, all of it in the workspace, where steps read it: what a stream or a graph orders between two steps is
+// then ordered for both the frequencies and the magnitude.
+struct StepRope {
+    double freq[64];          // radians per position; 0: not rotated
+    double magnitude;
+};
+// ... by a descriptor: theta^(-2i/128), or no rotation (theta 0)
+StepRope step_rope(float theta);
+
+// cos/sin of the rotary angles at position seq_len-1, times magnitude: table [batch][64]; optionally the step's plan.
+hipError_t launch_rope_table(const int32_t *seq_lens, const StepRope *rope, int max_tokens, int batch,
                              float2 *table, const AttnPlan *plan, hipStream_t s);
-// The 64 rotary frequencies, handed over as a kernel argument: no host-to-device copy.
-hipError_t launch_store_freq(const double *freq, double *dst, hipStream_t s);
+// Stored by a kernel, as its argument: no host-to-device copy.
+hipError_t launch_store_rope(const StepRope &rope, StepRope *dst, hipStream_t s);
 
 // Decode attention: RoPE of q, KV append and split-K partials (max, sum, weighted V) per workgroup ...
 hipError_t launch_attn(const float *qkv, const float2 *rope, KvView kv, int batch, int nq, int nkv, AttnSplit sp,

@@ -123,15 +123,13 @@ psv_status psv_set_rope(psv_ctx *c, const psv_rope *rope)
         if (!rope_ok(*rope)) return PSV_ERR_INVALID_ARG;
         if (rope->dims != PSV_HEAD_DIM || rope->pairing != PSV_ROPE_HALF) return PSV_ERR_UNSUPPORTED;
     }
-    if (rope || c->d.rope_theta > 0.f) {
-        double f[PSV_HEAD_DIM / 2];
-        for (int i = 0; i < (int)PSV_HEAD_DIM / 2; ++i) f[i] = rope ? rope->freq[i] : pow((double)c->d.rope_theta, -2.0 * (double)i / 128.0);
-        ST_TRY(check_stream(c->main));
-        HIP_TRY(launch_store_freq(f, c->at<double>(c->ws.inv_freq), c->main));
+    StepRope r = step_rope(c->d.rope_theta);
+    if (rope) {
+        memcpy(r.freq, rope->freq, sizeof r.freq);
+        r.magnitude = rope->magnitude;
     }
-    c->rope_set = rope != nullptr;
-    c->rope_magnitude = rope ? rope->magnitude : 1.0;
-    return PSV_OK;
+    ST_TRY(check_stream(c->main));
+    return launched(launch_store_rope(r, c->at<StepRope>(c->ws.rope_freq), c->main));
 }
 
 psv_status psv_rotate(const psv_rotate_args *a, const psv_rope *rope, void *stream)

@@ -72,11 +72,7 @@ extern "C" psv_status psv_decode_step_static(const psv_model_desc *desc, const p
         k2.v_pools = vp.data();
         ST_TRY(psv_set_kv(&c, &k2));
     }
-    if (desc->rope_theta > 0.f) {
-        double f[64];
-        for (int i = 0; i < 64; ++i) f[i] = pow((double)desc->rope_theta, -2.0 * (double)i / 128.0);
-        HIP_TRY(launch_store_freq(f, c.at<double>(ws.inv_freq), c.main));
-    }
+    HIP_TRY(launch_store_rope(step_rope(desc->rope_theta), c.at<StepRope>(ws.rope_freq), c.main));
     // Nothing in the workspace has to start at zero for a step without windows: every buffer is written by the step
     // before it is read (the flag words of the window fork are not used here), so the previous call's contents --
     // of this or any other shape -- are simply overwritten.
