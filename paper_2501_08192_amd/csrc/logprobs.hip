@@ -515,7 +515,8 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_join(JoinArgs g)
     }
     const float ln_s = logf(S);
     const bool none = top_order == kOrderNone;
-    auto answer = [&](float x) { return bad ? nan32() : none || x == -INFINITY ? -INFINITY : (x - M) * a.scale - ln_s; };
+    // by halves, whose difference is the exact half where that of the logits passes what 32 bits hold
+    auto answer = [&](float x) { return bad ? nan32() : none || x == -INFINITY ? -INFINITY : (0.5f * x - 0.5f * M) * (2.f * a.scale) - ln_s; };
     if (g.out.entropy && threadIdx.x == 0) g.out.entropy[row] = bad ? nan32() : none ? 0.f : ln_s - D * a.scale / S;
     if (g.out.logprobs && threadIdx.x < a.given) {
         const int32_t t = a.tokens[(size_t)row * a.given + threadIdx.x];

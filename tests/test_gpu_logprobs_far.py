@@ -103,3 +103,18 @@ def test_far_rows_in_the_largest_pieces(dtype):
     check_values(out[1], ent, spread, entropy=True)
     assert np.array_equal(out[3].numpy(), ids)
     check_values(out[2], best, spread)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1.0, 0.25, 2.0 ** -20, 2.0 ** -32])
+def test_logits_whose_difference_passes_32_bits(dtype, scale):
+    """A finite logit has a finite log probability wherever 32 bits hold it."""
+    x = logits(4, 5000, dtype, seed=13)
+    x[0, 10], x[0, 4000] = 3e38, -3e38
+    x[1, ::2], x[1, 1::2] = 3.3e38, -3.3e38
+    x[2, 4900] = -3.3e38
+    x[3] = torch.finfo(TYPES[dtype]).min
+    x[3, 1] = 2e38
+    tokens = torch.tensor([[10, 4000, 0, 4999]] * 4)
+    for kw in (dict(), dict(shards=[2500, 2500]), dict(shards=[1, 4999])):
+        check(x, tokens, scale, top=8, **kw)
