@@ -309,6 +309,11 @@ hipError_t launch_cache_append(const psv_append_args &a, const psv_cache &cache,
     g.turn_groups = (a.rows + g.turn_tile - 1) / g.turn_tile;
     g.column_tile = tile_of(a.rows * cache.n_kv_heads, kColumnTile);
     g.column_groups = columns ? (a.rows + g.column_tile - 1) / g.column_tile : 0;
+    // Both kinds together in one grid: with 2^24 rows and 2^28 kv heads at most, 2^22 of four rows and 2^23 + 128 of columns fit.
+    while (g.turn_groups + g.column_groups * cache.n_kv_heads > kMostGroups) {
+        g.turn_tile *= 2;
+        g.turn_groups = (a.rows + g.turn_tile - 1) / g.turn_tile;
+    }
     const bool half = !rope || rope->pairing == PSV_ROPE_HALF;
     if (a.dtype == PSV_F32) half ? launch_append_as<PSV_F32, true>(g, s) : launch_append_as<PSV_F32, false>(g, s);
     else if (a.dtype == PSV_BF16) half ? launch_append_as<PSV_BF16, true>(g, s) : launch_append_as<PSV_BF16, false>(g, s);
@@ -459,7 +464,8 @@ static void launch_gather_as(const GatherArgs &g, hipStream_t s)
 hipError_t launch_cache_gather(const psv_gather_args &a, const psv_cache &cache, hipStream_t s)
 {
     const bool columns = cache.kv_layout == PSV_KV_HEAD_MAJOR;
-    // four heads a lane of what lies as rows (16384 rows of 8 kv heads, token-major: 28.7 us, with 32 heads a lane 39.5)
+    // (A grid of all of them fits: one row a workgroup are 2^28 / 17 groups at most, token-major, or 2^28 / 33 and 2^23 + 33 of columns.)  Four
+    // heads a lane of what lies as rows (16384 rows of 8 kv heads, token-major: 28.7 us, with 32 heads a lane 39.5)
     const uint32_t most = 4 * (kRowThreads / 16) / (cache.n_kv_heads * (columns ? 1 : 2));
     GatherArgs g{a, cache, tile_of(a.rows, most < 1 ? 1 : most < (uint32_t)kColumnTile ? most : kColumnTile), 0, tile_of(a.rows * cache.n_kv_heads, kColumnTile), 0};
     g.row_groups = (a.rows + g.row_tile - 1) / g.row_tile;

@@ -10,7 +10,7 @@ using namespace psv;
 namespace {
 
 constexpr double kPi = 3.14159265358979323846;
-constexpr uint32_t kMostRows = 1u << 24, kMostHeads = 1u << 28;      // rows, and kv heads of all rows, of a call: what a grid of whole workgroups can name
+constexpr uint32_t kMostRows = 1u << 24, kMostHeads = 1u << 28;      // rows, and kv heads of all rows, of a call: what the launches divide into one grid
 
 size_t elem_size(uint32_t dtype) { return dtype == PSV_F32 ? 4 : 2; }
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }

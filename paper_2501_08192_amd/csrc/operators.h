@@ -7,6 +7,9 @@
 
 namespace psv {
 
+// A grid has fewer than 2^32 threads in a direction: workgroups of 256 in one launch.
+constexpr uint32_t kMostGroups = (1u << 24) - 1;
+
 hipError_t launch_rotate(const psv_rotate_args &a, const psv_rope &rope, bool vectors, hipStream_t s);
 hipError_t launch_cache_slots(const psv_slots_args &a, hipStream_t s);
 hipError_t launch_cache_append(const psv_append_args &a, const psv_cache &cache, const psv_rope *rope, hipStream_t s);

@@ -139,6 +139,7 @@ static void launch_rotate_as(RotateArgs &g, bool vectors, hipStream_t s)
     const uint32_t most = kRotateAngles / (dims / 2), want = 4 * g.slots / g.a.heads;
     g.tile = want < 1 ? 1 : want < most ? want : most;
     while (g.tile > 1 && g.a.rows / g.tile < 512) g.tile /= 2;
+    while ((g.a.rows + g.tile - 1) / g.tile > kMostGroups) g.tile *= 2;      // 2^24 rows, one a workgroup: two (at least eight have room for their angles)
     const dim3 grid((g.a.rows + g.tile - 1) / g.tile), block(kRotateThreads);
     if (half && vectors) PSV_LAUNCH((k_rotate<DT, true>), grid, block, 0, s, g);
     else if (half) PSV_LAUNCH((k_rotate_any<DT, true>), grid, block, 0, s, g);
