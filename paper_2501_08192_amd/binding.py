@@ -113,6 +113,7 @@ class psv_slots_args(C.Structure):
 
 
 class psv_cache(C.Structure):
+    device = None      # of the pools, where they were given as tensors
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("n_kv_heads", C.c_uint32), ("kv_format", C.c_uint32),
                 ("kv_layout", C.c_uint32), ("num_pool_blocks", C.c_uint32)]
 
@@ -453,6 +454,19 @@ def _dtype(name, t):
     return code
 
 
+def _device(stream, t):
+    """The GPU that a call's tensors lie on: its stream's, or, of a stream that is only a handle, that of its first tensor."""
+    at = getattr(stream, "device_index", None)
+    return t.get_device() if at is None else at
+
+
+def _place(name, t, at):
+    """The address of a tensor on GPU `at`: kernels follow it."""
+    if t.get_device() != at or at < 0:
+        raise ValueError("%s: a tensor on the stream's GPU is wanted, got one on %s" % (name, t.device))
+    return t.data_ptr()
+
+
 def _rows(name, t):
     """(dtype code, row stride, shape) of rows [rows, heads, channels] whose heads and channels are adjacent."""
     shape, stride = t.shape, t.stride()
@@ -461,11 +475,20 @@ def _rows(name, t):
     return _dtype(name, t), stride[0], shape
 
 
-def _want(name, t, dtype, *shape):
-    """The address of a contiguous tensor of a type and shape."""
+def _want(name, t, at, dtype, *shape):
+    """The address of a contiguous tensor of a type and shape on GPU `at`."""
     if (_TYPES.get(t.dtype) or _type(t)) != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: contiguous %s %s is wanted, got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
-    return t.data_ptr()
+    return _place(name, t, at)
+
+
+def _bytes_at(name, t, at, n):
+    """The address of a contiguous tensor of `n` bytes or more; nothing for none."""
+    if t is None and n == 0:
+        return None
+    if not t.is_contiguous() or t.numel() * t.element_size() < n:
+        raise ValueError("%s: a contiguous tensor of at least %d bytes is wanted, got %s of %s" % (name, n, list(t.shape), t.dtype))
+    return _place(name, t, at)
 
 
 def psv_rope_plan(dims=128, pairing="half", theta=500000.0, scaling="plain", factor=1.0, low_turns=1.0, high_turns=4.0,
@@ -486,7 +509,8 @@ def psv_rotate(x, y, positions, rope, stream, transpose=False):
     shape, xs, ys = x.shape, x.stride(), y.stride()
     if len(shape) != 3 or y.shape != shape or y.dtype != x.dtype or (shape[2] > 1 and (xs[2] != 1 or ys[2] != 1)):
         raise ValueError("psv_rotate: x and y of one shape [rows, heads, channels] and type with adjacent channels are wanted")
-    a = psv_rotate_args(x.data_ptr(), y.data_ptr(), _want("positions", positions, "int32", shape[0]), shape[0], shape[1], shape[2], _dtype("x", x),
+    at = _device(stream, x)
+    a = psv_rotate_args(_place("x", x, at), _place("y", y, at), _want("positions", positions, at, "int32", shape[0]), shape[0], shape[1], shape[2], _dtype("x", x),
                         1 if transpose else 0, 0, xs[0], xs[1], ys[0], ys[1])
     _check(lib().psv_rotate(C.byref(a), C.byref(rope), _stream(stream)), "psv_rotate")
 
@@ -498,19 +522,33 @@ def psv_cache_slots(lens, new_lens, block_table, free_blocks, free_range, num_po
     n, rows = lens.shape[0], slots.shape[0]
     table = block_table is not None
     mb, n_free = (block_table.shape[-1], free_blocks.shape[0]) if table else (int(max_blocks), 0)
-    a = psv_slots_args(_want("lens", lens, "int32", n), _want("new_lens", new_lens, "int32", n),
-                       _want("block_table", block_table, "int32", n, mb) if table else None,
-                       _want("free_blocks", free_blocks, "int32", n_free) if table else None,
-                       _want("free_range", free_range, "int32", 2) if table else None, n_free, n, mb, num_pool_blocks, rows, 0, _want("seq_lens", seq_lens, "int32", n), _want("row_starts", row_starts, "int32", n + 1),
-                       _want("slots", slots, "int64", rows), _want("positions", positions, "int32", rows),
-                       _want("requests", requests, "int32", rows), _want("free_range_out", free_range_out, "int32", 2) if table else None,
-                       _want("refused", refused, "int32", 1))
+    at = _device(stream, lens)
+    a = psv_slots_args(_want("lens", lens, at, "int32", n), _want("new_lens", new_lens, at, "int32", n),
+                       _want("block_table", block_table, at, "int32", n, mb) if table else None,
+                       _want("free_blocks", free_blocks, at, "int32", n_free) if table else None,
+                       _want("free_range", free_range, at, "int32", 2) if table else None, n_free, n, mb, num_pool_blocks, rows, 0,
+                       _want("seq_lens", seq_lens, at, "int32", n), _want("row_starts", row_starts, at, "int32", n + 1),
+                       _want("slots", slots, at, "int64", rows), _want("positions", positions, at, "int32", rows),
+                       _want("requests", requests, at, "int32", rows),
+                       _want("free_range_out", free_range_out, at, "int32", 2) if table else None, _want("refused", refused, at, "int32", 1))
     _check(lib().psv_cache_slots(C.byref(a), _stream(stream)), "psv_cache_slots")
 
 
 def kv_cache(k_pool, v_pool, n_kv_heads, kv_format, kv_layout, num_pool_blocks):
-    """One layer's pools; kv_format, kv_layout: keys of FORMATS and KV_LAYOUTS."""
-    return psv_cache(_dev_ptr(k_pool), _dev_ptr(v_pool), n_kv_heads, FORMATS[kv_format], KV_LAYOUTS[kv_layout], num_pool_blocks)
+    """One layer's pools, tensors on one GPU or addresses; kv_format, kv_layout: keys of FORMATS and KV_LAYOUTS."""
+    at = None
+    for name, t in (("k_pool", k_pool), ("v_pool", v_pool)):
+        if t is not None and not isinstance(t, int):
+            at = t.get_device() if at is None else at
+            _place(name, t, at)
+    cache = psv_cache(_dev_ptr(k_pool), _dev_ptr(v_pool), n_kv_heads, FORMATS[kv_format], KV_LAYOUTS[kv_layout], num_pool_blocks)
+    cache.device = at
+    return cache
+
+
+def _same_gpu(cache, at):
+    if cache.device is not None and cache.device != at:
+        raise ValueError("cache: its pools lie on GPU %d, the call's tensors on GPU %d" % (cache.device, at))
 
 
 def psv_cache_append(q, k, v, q_out, positions, slots, cache, rope, stream):
@@ -519,15 +557,17 @@ def psv_cache_append(q, k, v, q_out, positions, slots, cache, rope, stream):
     dv, v_row, v_shape = _rows("v", v)
     if dv != dt or v_shape != shape or shape[1] != cache.n_kv_heads:
         raise ValueError("psv_cache_append: k and v of one type with the cache's %d heads are wanted" % cache.n_kv_heads)
+    at = _device(stream, k)
     rows, nq, q_row, q_out_row, q_at, q_out_at = shape[0], 0, 0, 0, None, None
     if q is not None:
         dq, q_row, q_shape = _rows("q", q)
         do, q_out_row, q_out_shape = _rows("q_out", q_out)
         if dq != dt or do != dt or q_out_shape != q_shape or q_shape[0] != rows:
             raise ValueError("psv_cache_append: q and q_out of k's type and rows are wanted")
-        nq, q_at, q_out_at = q_shape[1], q.data_ptr(), q_out.data_ptr()
-    a = psv_append_args(q_at, k.data_ptr(), v.data_ptr(), q_out_at, None if positions is None else _want("positions", positions, "int32", rows),
-                        _want("slots", slots, "int64", rows), rows, nq, dt, 0, q_row, k_row, v_row, q_out_row)
+        nq, q_at, q_out_at = q_shape[1], _place("q", q, at), _place("q_out", q_out, at)
+    _same_gpu(cache, at)
+    a = psv_append_args(q_at, _place("k", k, at), _place("v", v, at), q_out_at,
+                        None if positions is None else _want("positions", positions, at, "int32", rows), _want("slots", slots, at, "int64", rows), rows, nq, dt, 0, q_row, k_row, v_row, q_out_row)
     _check(lib().psv_cache_append(C.byref(a), C.byref(cache), None if rope is None else C.byref(rope), _stream(stream)), "psv_cache_append")
 
 
@@ -538,7 +578,9 @@ def psv_cache_gather(slots, k, v, cache, stream):
     dv, v_row, v_shape = _rows("v", v)
     if dv != dt or v_shape != shape or shape[0] != rows or shape[1] != cache.n_kv_heads:
         raise ValueError("psv_cache_gather: k and v of one type with %d rows of the cache's %d heads are wanted" % (rows, cache.n_kv_heads))
-    a = psv_gather_args(_want("slots", slots, "int64", rows), k.data_ptr(), v.data_ptr(), rows, dt, k_row, v_row)
+    at = _device(stream, k)
+    _same_gpu(cache, at)
+    a = psv_gather_args(_want("slots", slots, at, "int64", rows), _place("k", k, at), _place("v", v, at), rows, dt, k_row, v_row)
     _check(lib().psv_cache_gather(C.byref(a), C.byref(cache), _stream(stream)), "psv_cache_gather")
 
 
@@ -550,55 +592,51 @@ def psv_logprobs_bytes(rows, records, given, top):
     return int(lib().psv_logprobs_bytes(rows, records, given, top))
 
 
-def _logprobs_args(rows, logits, tokens, scale, top, first_token, vocab, records):
+def _logprobs_args(at, rows, logits, tokens, scale, top, first_token, vocab, records):
     given = 0 if tokens is None else tokens.shape[1]
-    columns, row, dt = 0, 0, PSV_F32
+    columns, row, dt, where = 0, 0, PSV_F32, None
     if logits is not None:
         shape, stride = logits.shape, logits.stride()
         if len(shape) != 2 or shape[0] != rows or (shape[1] > 1 and stride[1] != 1):
             raise ValueError("logits: [rows, columns] with adjacent columns are wanted")
-        columns, row, dt = shape[1], stride[0], _dtype("logits", logits)
-    return psv_logprobs_args(_dev_ptr(logits), None if given == 0 else _want("tokens", tokens, "int32", rows, given), rows, columns, first_token,
+        columns, row, dt, where = shape[1], stride[0], _dtype("logits", logits), _place("logits", logits, at)
+    return psv_logprobs_args(where, None if given == 0 else _want("tokens", tokens, at, "int32", rows, given), rows, columns, first_token,
                              columns if vocab is None else vocab, dt, given, top, scale, records, 0, row)
 
 
-def _logprobs_out(rows, given, logprobs, entropy, top_logprobs, top_ids):
+def _logprobs_out(at, rows, given, logprobs, entropy, top_logprobs, top_ids):
     top = 0 if top_ids is None else top_ids.shape[1]
-    return psv_logprobs_out(None if logprobs is None else _want("logprobs", logprobs, "float32", rows, given),
-                            None if entropy is None else _want("entropy", entropy, "float32", rows),
-                            None if top == 0 else _want("top_logprobs", top_logprobs, "float32", rows, top),
-                            None if top == 0 else _want("top_ids", top_ids, "int32", rows, top)), top
-
-
-def _bytes_of(t):
-    return t.numel() * t.element_size()
+    return psv_logprobs_out(None if logprobs is None else _want("logprobs", logprobs, at, "float32", rows, given),
+                            None if entropy is None else _want("entropy", entropy, at, "float32", rows),
+                            None if top == 0 else _want("top_logprobs", top_logprobs, at, "float32", rows, top),
+                            None if top == 0 else _want("top_ids", top_ids, at, "int32", rows, top)), top
 
 
 def psv_logprobs_part(logits, tokens, scale, top, records_out, stream, first_token=0, vocab=None, records=0):
-    """logits [rows, columns]: a shard's columns of the vocabulary; tokens int32 [rows, given] or None; records_out: a tensor of at least
-    psv_logprobs_bytes bytes."""
-    rows = logits.shape[0]
-    a = _logprobs_args(rows, logits, tokens, scale, top, first_token, vocab, records)
-    if rows and _bytes_of(records_out) < psv_logprobs_bytes(rows, records or psv_logprobs_records(rows, a.columns), a.given, top):
-        raise ValueError("psv_logprobs_part: the records do not fit their tensor")
-    _check(lib().psv_logprobs_part(C.byref(a), _dev_ptr(records_out), _stream(stream)), "psv_logprobs_part")
+    """logits [rows, columns]: a shard's columns of the vocabulary; tokens int32 [rows, given] or None; records_out: a contiguous tensor of at
+    least psv_logprobs_bytes bytes."""
+    rows, at = logits.shape[0], _device(stream, logits)
+    a = _logprobs_args(at, rows, logits, tokens, scale, top, first_token, vocab, records)
+    size = psv_logprobs_bytes(rows, records or psv_logprobs_records(rows, a.columns), a.given, top)
+    _check(lib().psv_logprobs_part(C.byref(a), _bytes_at("records_out", records_out, at, size), _stream(stream)), "psv_logprobs_part")
 
 
 def psv_logprobs_join(rows, tokens, scale, vocab, records, shards, logprobs, entropy, top_logprobs, top_ids, records_in, stream, top=None):
     """records_in: the shards' records of psv_logprobs_part behind one another; top: of the records (top_ids's width by default)."""
-    out, n = _logprobs_out(rows, 0 if tokens is None else tokens.shape[1], logprobs, entropy, top_logprobs, top_ids)
+    at = _device(stream, records_in)
+    out, n = _logprobs_out(at, rows, 0 if tokens is None else tokens.shape[1], logprobs, entropy, top_logprobs, top_ids)
     if top is not None and n not in (0, top):
         raise ValueError("psv_logprobs_join: top_ids is [rows, top]")
-    a = _logprobs_args(rows, None, tokens, scale, n if top is None else top, 0, vocab, records)
-    if rows and _bytes_of(records_in) < shards * psv_logprobs_bytes(rows, records, a.given, a.top):
-        raise ValueError("psv_logprobs_join: %d shards of %d records a row are wanted" % (shards, records))
-    _check(lib().psv_logprobs_join(C.byref(a), _dev_ptr(records_in), shards, C.byref(out), _stream(stream)), "psv_logprobs_join")
+    a = _logprobs_args(at, rows, None, tokens, scale, n if top is None else top, 0, vocab, records)
+    size = shards * psv_logprobs_bytes(rows, records, a.given, a.top)
+    _check(lib().psv_logprobs_join(C.byref(a), _bytes_at("records_in", records_in, at, size), shards, C.byref(out), _stream(stream)), "psv_logprobs_join")
 
 
 def psv_logprobs(logits, tokens, scale, logprobs, entropy, top_logprobs, top_ids, workspace, stream):
-    """logits [rows, vocabulary]; tokens int32 [rows, given] or None; the outputs, any of them None; workspace: a tensor of at least
+    """logits [rows, vocabulary]; tokens int32 [rows, given] or None; the outputs, any of them None; workspace: a contiguous tensor of at least
     psv_logprobs_bytes bytes."""
-    rows = logits.shape[0]
-    out, top = _logprobs_out(rows, 0 if tokens is None else tokens.shape[1], logprobs, entropy, top_logprobs, top_ids)
-    a = _logprobs_args(rows, logits, tokens, scale, top, 0, None, 0)
-    _check(lib().psv_logprobs(C.byref(a), C.byref(out), _dev_ptr(workspace), _bytes_of(workspace), _stream(stream)), "psv_logprobs")
+    rows, at = logits.shape[0], _device(stream, logits)
+    out, top = _logprobs_out(at, rows, 0 if tokens is None else tokens.shape[1], logprobs, entropy, top_logprobs, top_ids)
+    a = _logprobs_args(at, rows, logits, tokens, scale, top, 0, None, 0)
+    _check(lib().psv_logprobs(C.byref(a), C.byref(out), _bytes_at("workspace", workspace, at, 0), workspace.numel() * workspace.element_size(),
+                              _stream(stream)), "psv_logprobs")
