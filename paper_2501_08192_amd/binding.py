@@ -605,6 +605,8 @@ def _logprobs_args(at, rows, logits, tokens, scale, top, first_token, vocab, rec
 
 
 def _logprobs_out(at, rows, given, logprobs, entropy, top_logprobs, top_ids):
+    if (top_ids is None) != (top_logprobs is None):
+        raise ValueError("top_logprobs, top_ids: both or neither are wanted")
     top = 0 if top_ids is None else top_ids.shape[1]
     return psv_logprobs_out(None if logprobs is None else _want("logprobs", logprobs, at, "float32", rows, given),
                             None if entropy is None else _want("entropy", entropy, at, "float32", rows),
@@ -633,8 +635,8 @@ def psv_logprobs_join(rows, tokens, scale, vocab, records, shards, logprobs, ent
 
 
 def psv_logprobs(logits, tokens, scale, logprobs, entropy, top_logprobs, top_ids, workspace, stream):
-    """logits [rows, vocabulary]; tokens int32 [rows, given] or None; the outputs, any of them None; workspace: a contiguous tensor of at least
-    psv_logprobs_bytes bytes."""
+    """logits [rows, vocabulary]; tokens int32 [rows, given] or None; the outputs, any of them None, top_logprobs and top_ids together;
+    workspace: a contiguous tensor of at least psv_logprobs_bytes bytes."""
     rows, at = logits.shape[0], _device(stream, logits)
     out, top = _logprobs_out(at, rows, 0 if tokens is None else tokens.shape[1], logprobs, entropy, top_logprobs, top_ids)
     a = _logprobs_args(at, rows, logits, tokens, scale, top, 0, None, 0)

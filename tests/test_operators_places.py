@@ -114,3 +114,15 @@ def test_records_whose_memory_is_smaller_than_their_size_are_refused(name, libra
 def test_no_rows_need_no_records(library):
     psv.psv_logprobs_part(torch.zeros(0, V).as_subclass(On0), None, 1.0, 4, None, None)
     assert library.calls == 1
+
+
+@pytest.mark.parametrize("name", ["join", "logprobs"])
+def test_alternatives_are_ids_and_log_probabilities_together(name, library):
+    """The one without the other would be left as it was, without a word."""
+    tensors, call = CALLS[name]
+    there = {k: t.as_subclass(On0) for k, t in tensors.items()}
+    for missing in ("top_ids", "top_logprobs"):
+        with pytest.raises(ValueError, match="both or neither"):
+            call(dict(there, **{missing: None}), None)
+    call(dict(there, top_ids=None, top_logprobs=None), None)
+    assert library.calls == 1
