@@ -460,26 +460,35 @@ def _device(stream, t):
     return t.get_device() if at is None else at
 
 
+def _elsewhere(name, t):
+    raise ValueError("%s: a tensor on the stream's GPU is wanted, got one on %s" % (name, t.device))
+
+
 def _place(name, t, at):
     """The address of a tensor on GPU `at`: kernels follow it."""
     if t.get_device() != at or at < 0:
-        raise ValueError("%s: a tensor on the stream's GPU is wanted, got one on %s" % (name, t.device))
+        _elsewhere(name, t)
     return t.data_ptr()
 
 
-def _rows(name, t):
-    """(dtype code, row stride, shape) of rows [rows, heads, channels] whose heads and channels are adjacent."""
+def _rows(name, t, at):
+    """(dtype code, row stride, shape, address) of rows [rows, heads, channels] on GPU `at` whose heads and channels are adjacent."""
     shape, stride = t.shape, t.stride()
     if len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or (shape[1] > 1 and stride[1] != 128):
         raise ValueError("%s: rows of [heads][128] adjacent elements are wanted, got shape %s, strides %s" % (name, tuple(shape), stride))
-    return _dtype(name, t), stride[0], shape
+    if t.get_device() != at or at < 0:
+        _elsewhere(name, t)
+    code = _ROW_CODES.get(t.dtype)
+    return _dtype(name, t) if code is None else code, stride[0], shape, t.data_ptr()
 
 
 def _want(name, t, at, dtype, *shape):
     """The address of a contiguous tensor of a type and shape on GPU `at`."""
     if (_TYPES.get(t.dtype) or _type(t)) != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: contiguous %s %s is wanted, got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
-    return _place(name, t, at)
+    if t.get_device() != at or at < 0:
+        _elsewhere(name, t)
+    return t.data_ptr()
 
 
 def _bytes_at(name, t, at, n):
@@ -536,51 +545,53 @@ def psv_cache_slots(lens, new_lens, block_table, free_blocks, free_range, num_po
 
 def kv_cache(k_pool, v_pool, n_kv_heads, kv_format, kv_layout, num_pool_blocks):
     """One layer's pools, tensors on one GPU or addresses; kv_format, kv_layout: keys of FORMATS and KV_LAYOUTS."""
-    at = None
-    for name, t in (("k_pool", k_pool), ("v_pool", v_pool)):
-        if t is not None and not isinstance(t, int):
-            at = t.get_device() if at is None else at
-            _place(name, t, at)
-    cache = psv_cache(_dev_ptr(k_pool), _dev_ptr(v_pool), n_kv_heads, FORMATS[kv_format], KV_LAYOUTS[kv_layout], num_pool_blocks)
+    if k_pool is None or v_pool is None or isinstance(k_pool, int) or isinstance(v_pool, int):
+        for t in (k_pool, v_pool):
+            if t is not None and not isinstance(t, int):
+                _place("pool", t, t.get_device())
+        return psv_cache(_dev_ptr(k_pool), _dev_ptr(v_pool), n_kv_heads, FORMATS[kv_format], KV_LAYOUTS[kv_layout], num_pool_blocks)
+    at = k_pool.get_device()
+    cache = psv_cache(_place("k_pool", k_pool, at), _place("v_pool", v_pool, at), n_kv_heads, FORMATS[kv_format], KV_LAYOUTS[kv_layout], num_pool_blocks)
     cache.device = at
     return cache
 
 
-def _same_gpu(cache, at):
-    if cache.device is not None and cache.device != at:
-        raise ValueError("cache: its pools lie on GPU %d, the call's tensors on GPU %d" % (cache.device, at))
+def _other_gpu(cache, at):
+    raise ValueError("cache: its pools lie on GPU %d, the call's tensors on GPU %d" % (cache.device, at))
 
 
 def psv_cache_append(q, k, v, q_out, positions, slots, cache, rope, stream):
     """q, q_out [rows, q heads, 128], or None; k, v [rows, kv heads, 128]; positions int32 [rows] (None without rope); slots int64 [rows]."""
-    dt, k_row, shape = _rows("k", k)
-    dv, v_row, v_shape = _rows("v", v)
+    at = _device(stream, k)
+    dt, k_row, shape, k_at = _rows("k", k, at)
+    dv, v_row, v_shape, v_at = _rows("v", v, at)
     if dv != dt or v_shape != shape or shape[1] != cache.n_kv_heads:
         raise ValueError("psv_cache_append: k and v of one type with the cache's %d heads are wanted" % cache.n_kv_heads)
-    at = _device(stream, k)
     rows, nq, q_row, q_out_row, q_at, q_out_at = shape[0], 0, 0, 0, None, None
     if q is not None:
-        dq, q_row, q_shape = _rows("q", q)
-        do, q_out_row, q_out_shape = _rows("q_out", q_out)
+        dq, q_row, q_shape, q_at = _rows("q", q, at)
+        do, q_out_row, q_out_shape, q_out_at = _rows("q_out", q_out, at)
         if dq != dt or do != dt or q_out_shape != q_shape or q_shape[0] != rows:
             raise ValueError("psv_cache_append: q and q_out of k's type and rows are wanted")
-        nq, q_at, q_out_at = q_shape[1], _place("q", q, at), _place("q_out", q_out, at)
-    _same_gpu(cache, at)
-    a = psv_append_args(q_at, _place("k", k, at), _place("v", v, at), q_out_at,
-                        None if positions is None else _want("positions", positions, at, "int32", rows), _want("slots", slots, at, "int64", rows), rows, nq, dt, 0, q_row, k_row, v_row, q_out_row)
+        nq = q_shape[1]
+    if cache.device != at and cache.device is not None:
+        _other_gpu(cache, at)
+    a = psv_append_args(q_at, k_at, v_at, q_out_at, None if positions is None else _want("positions", positions, at, "int32", rows),
+                        _want("slots", slots, at, "int64", rows), rows, nq, dt, 0, q_row, k_row, v_row, q_out_row)
     _check(lib().psv_cache_append(C.byref(a), C.byref(cache), None if rope is None else C.byref(rope), _stream(stream)), "psv_cache_append")
 
 
 def psv_cache_gather(slots, k, v, cache, stream):
     """slots int64 [rows]; k, v [rows, kv heads, 128] of one type."""
     rows = slots.shape[0]
-    dt, k_row, shape = _rows("k", k)
-    dv, v_row, v_shape = _rows("v", v)
+    at = _device(stream, k)
+    dt, k_row, shape, k_at = _rows("k", k, at)
+    dv, v_row, v_shape, v_at = _rows("v", v, at)
     if dv != dt or v_shape != shape or shape[0] != rows or shape[1] != cache.n_kv_heads:
         raise ValueError("psv_cache_gather: k and v of one type with %d rows of the cache's %d heads are wanted" % (rows, cache.n_kv_heads))
-    at = _device(stream, k)
-    _same_gpu(cache, at)
-    a = psv_gather_args(_want("slots", slots, at, "int64", rows), _place("k", k, at), _place("v", v, at), rows, dt, k_row, v_row)
+    if cache.device != at and cache.device is not None:
+        _other_gpu(cache, at)
+    a = psv_gather_args(_want("slots", slots, at, "int64", rows), k_at, v_at, rows, dt, k_row, v_row)
     _check(lib().psv_cache_gather(C.byref(a), C.byref(cache), _stream(stream)), "psv_cache_gather")
 
 

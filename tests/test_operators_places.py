@@ -126,3 +126,36 @@ def test_alternatives_are_ids_and_log_probabilities_together(name, library):
             call(dict(there, **{missing: None}), None)
     call(dict(there, top_ids=None, top_logprobs=None), None)
     assert library.calls == 1
+
+
+def test_shapes_types_and_strides_of_tensors_that_lie_right_are_checked_as_well(library):
+    f, i, l = (t.as_subclass(On0) for t in (torch.zeros(2, 3, 128), torch.zeros(2, dtype=torch.int32), torch.zeros(2, dtype=torch.int64)))
+    three, two = (psv.kv_cache(1 << 20, 1 << 20, n, "bf16", "head", 4) for n in (3, 2))
+    x, t12 = f[0], i.reshape(1, 2)
+    calls = [
+        (lambda: psv.psv_rotate(f, f.double(), i, ROPE, None), "one shape"),
+        (lambda: psv.psv_rotate(f, f, l, ROPE, None), "positions"),
+        (lambda: psv.psv_rotate(f.transpose(1, 2), f.transpose(1, 2), i, ROPE, None), "adjacent"),
+        (lambda: psv.psv_rotate(f, f, i[:1], ROPE, None), "positions"),
+        (lambda: psv.psv_cache_gather(i, f, f, three, None), "slots"),
+        (lambda: psv.psv_cache_gather(l, f, f, two, None), "heads"),
+        (lambda: psv.psv_cache_gather(l, f, f[:, :2], three, None), "heads"),
+        (lambda: psv.psv_cache_gather(l, f, f.transpose(1, 2), three, None), "adjacent"),
+        (lambda: psv.psv_cache_append(None, f, f[:, :2], None, i, l, three, ROPE, None), "heads"),
+        (lambda: psv.psv_cache_append(f, f, f, f[:1], i, l, three, ROPE, None), "rows"),
+        (lambda: psv.psv_cache_append(f, f, f, f.half(), i, l, three, ROPE, None), "type"),
+        (lambda: psv.psv_cache_append(None, f, f, None, i, i, three, ROPE, None), "slots"),
+        (lambda: psv.psv_cache_append(None, f.int(), f.int(), None, i, l, three, ROPE, None), "float32"),
+        (lambda: psv.psv_logprobs(x.t(), None, 1.0, None, None, None, None, f, None), "adjacent"),
+        (lambda: psv.psv_logprobs(x, t12, 1.0, None, None, None, None, f, None), "tokens"),
+        (lambda: psv.psv_logprobs_part(x, None, 1.0, 4, i, None), "bytes"),
+        (lambda: psv.psv_logprobs_join(3, None, 1.0, 128, 1, 2, None, None, None, None, i, None, top=4), "bytes"),
+    ]
+    for call, what in calls:
+        with pytest.raises(ValueError, match=what):
+            call()
+    assert library.calls == 0
+    for pools in ((1 << 20, f[0, 0]), (f[0, 0], 1 << 20)):
+        psv.kv_cache(*pools, 1, "bf16", "head", 4)
+        with pytest.raises(ValueError, match="GPU"):
+            psv.kv_cache(*(p if isinstance(p, int) else torch.zeros(8) for p in pools), 1, "bf16", "head", 4)
