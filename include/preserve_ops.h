@@ -63,12 +63,13 @@ typedef struct {
 /* Pure host function. */
 psv_status psv_rope_plan(const psv_rope_desc *desc, psv_rope *out);
 
-/* The decode steps of this context (psv_decode_step) that run after this on stream_main rotate with these frequencies and this magnitude instead
- * of the descriptor's rope_theta (rope = NULL: with the descriptor's again).  A step rotates whole heads in halves: dims = 128 and
- * PSV_ROPE_HALF, else PSV_ERR_UNSUPPORTED (a model of other pairs is served by permuting the rows of its query and key
- * projections: the product of a query and a key does not depend on the order of the channels; unrotated channels are pairs of
- * frequency 0).  Both travel as a kernel argument on stream_main into the context's workspace, where a step reads them: ordered with the steps, nothing
- * is awaited.  A captured call takes effect when its graph runs, and a step that a graph holds rotates with what was set last when it runs. */
+/* The decode steps of this context (psv_decode_step) that run after this on stream_main rotate with these frequencies and this magnitude
+ * instead of the descriptor's rope_theta (rope = NULL: with the descriptor's again).  psv_decode_step_static has no context and goes by its
+ * descriptor.  A step rotates whole heads in halves: dims = 128 and PSV_ROPE_HALF, else PSV_ERR_UNSUPPORTED (a model of other pairs is served by
+ * permuting the rows of its query and key projections: the product of a query and a key does not depend on the order of the channels; unrotated
+ * channels are pairs of frequency 0, which a magnitude other than 1 would scale as well).  Both travel as a kernel argument on stream_main into
+ * the context's workspace, where a step reads them: ordered with the steps, nothing is awaited.  A captured call takes effect when its graph
+ * runs, and a step that a graph holds rotates with what was set last when it runs. */
 psv_status psv_set_rope(psv_ctx *ctx, const psv_rope *rope);
 
 /* Rotates rows: y = x with the first rope->dims channels of every head rotated to the row's position, computed in 32 bits (angles
