@@ -96,11 +96,13 @@ psv_status psv_rotate(const psv_rotate_args *a, const psv_rope *rope, void *stre
  * new_lens[b] more (>= 0; 1 in a decode step, a prompt or a part of one otherwise); their rows follow one another, request by request,
  * in the step's row arrays.  Blocks that a request needs beyond those that hold its lens[b] tokens are taken from the free list, in
  * request order, and entered into its row of the block table.
- * A request is refused -- it keeps its length, takes no block, and its rows get slot -1 -- when a length is negative, lens + new_lens
+ * A request is refused -- it keeps its length, takes no block, and its rows get slot -1, which append and gather skip -- when a length is negative, lens + new_lens
  * exceeds max_blocks * 16, its rows do not fit `rows`, or it needs blocks and the free list does not hold those of all requests up to it
  * (refused ones of the other kinds need none).  A negative new length stands for no rows.
  * Slot of the token at position p of request b: block_table[b][p / 16] * 16 + p % 16 -- what psv_cache_append and psv_cache_gather take --
  * or -1 where the block's id is not in [0, num_pool_blocks).
+ * A decode step knows lengths alone: one over a refused request's kept length would write the new token over the last cached one.  Its seq_lens are
+ * 0 there (an empty sequence, whose cache a step leaves alone); with one row a request, seq_lens[b] where slots[b] >= 0 and 0 elsewhere.
  * Nothing read is written (block_table apart, whose entries of held blocks are read and whose new ones are written), so a repeated call
  * gives the same answers; a program alternates between two sets of lens / seq_lens and free_range / free_range_out. */
 typedef struct {
@@ -115,7 +117,7 @@ typedef struct {
     uint32_t num_pool_blocks;
     uint32_t rows;                /* entries of the row arrays */
     uint32_t reserved;
-    int32_t *seq_lens;            /* dev [batch] out: lens + new_lens, or lens where refused: psv_kv_desc's seq_lens of a decode step */
+    int32_t *seq_lens;            /* dev [batch] out: lens + new_lens, or lens where refused; psv_kv_desc's seq_lens of a decode step in which none was */
     int32_t *row_starts;          /* dev [batch + 1] out: first row of each request and the end of the last, at most `rows` */
     int64_t *slots;               /* dev [rows] out; -1 for rows of refused requests and behind the last */
     int32_t *positions;           /* dev [rows] out: lens + place within the request, refused ones included; 0 behind the last row */
