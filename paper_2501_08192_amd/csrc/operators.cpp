@@ -205,8 +205,9 @@ uint32_t psv_logprobs_records(uint32_t rows, uint32_t columns)
 {
     if (rows > (1u << 20) || columns == 0 || columns > (1u << 21)) return 0;
     // The largest pieces, which cost least a column, that still give every compute unit one; below 4096 columns the records cost
-    // more than the pieces gain.  (128256 columns in bf16, pieces of 16384 / 8192 / 4096 / 2048: 256 rows 28.1 / 33.5 / 45.5 / 69.8 us, 64
-    // rows 17.2 / 18.3 / 22.0 / 29.6, 8 rows 13.7 / 12.8 / 12.8 / 16.1; 61 rows of 32003 13.4 / 12.2 / 11.8 / 13.4.)
+    // more than the pieces gain.  (Both kernels of calls in a stream for 8 alternatives, pieces of 16384 / 8192 / 4096 / 2048: of 128256 columns in bf16
+    // 256 rows 26.4 / 28.8 / 37.5 / 58.8 us, 64 rows 14.6 / 15.0 / 17.5 / 23.2, 8 rows 10.6 / 10.2 / 10.5 / 11.2; 61 rows of 32003 in f16 11.6 / 11.0 / 11.2 /
+    // 12.3.)
     uint32_t most = kLogprobThreads * 64;
     while (most > 4096 && (uint64_t)rows * ((columns + most - 1) / most) < 256 && (columns + most / 2 - 1) / (most / 2) <= PSV_LOGPROBS_MAX_RECORDS) most /= 2;
     return (columns + most - 1) / most;
@@ -238,9 +239,12 @@ psv_status psv_logprobs(const psv_logprobs_args *a, const psv_logprobs_out *out,
 {
     psv_logprobs_args b;
     ST_TRY(part_args(a, workspace, &b));
-    // Pieces of twice the size, where there are thousands, two columns fit a register and alternatives are wanted: what a piece costs beside its
-    // columns is halved (2048 rows of 128256 in bf16, none / 8 / 20 alternatives: 97.3 / 100.6 / 107.5 us against 93.6 / 102.0 / 111.1; 256
-    // rows 17.9 / 21.1 / 21.9 against 16.6 / 20.4 / 22.0).  These are fewer records than the workspace has room for.
+    // Pieces of twice the size, where there are thousands, two columns fit a register and alternatives are wanted: half as many records to join and to
+    // choose from, against half as many waves at once.  (Both kernels of calls in a stream.  Rows in which a dozen logits stand out, 8 alternatives: 2048
+    // rows of 128256 in bf16 109 us against 113, 512 rows 39.1 against 38.0, 2048 rows of 32000 40.1 against 40.6, 4096 in f16 62.3 against 65.1; more
+    // padding costs: 2048 rows of 200000 177 against 172.  Rows without, 4 / 8 / 20 / 32 alternatives: 2048 rows of 128256 108.9 / 110.4 / 114.9 / 125.8
+    // against 109.0 / 109.4 / 117.4 / 134.4, 512 rows 40.8 / 41.2 / 42.1 / 48.7 against 38.4 / 38.4 / 41.9 / 53.3.)  These are fewer records than the
+    // workspace has room for.
     const uint32_t fewer = (b.columns + kLogprobMostColumns - 1) / kLogprobMostColumns;
     if (a->records == 0 && b.dtype != PSV_F32 && b.top >= 8 && fewer < b.records && (uint64_t)b.rows * fewer >= 2048) b.records = fewer;
     if (b.first_token != 0 || b.columns != b.vocab || workspace_bytes < psv_logprobs_bytes(b.rows, b.records, b.given, b.top)) return PSV_ERR_INVALID_ARG;
