@@ -5,8 +5,8 @@
 // of 128 lines.  Its rows go through LDS, and where eight of them follow one another from a slot that is a multiple of eight on -- all of a
 // prompt but its ends -- a lane moves one channel of the eight at once.  Such an octet belongs to the workgroup that has its first row, so that
 // where tiles of rows end does not matter.  The two kinds of work are workgroups of their own, side by side in one launch.
-// (Append of 9500 rows of 8 query and 2 kv heads, 58 MB: 11.5 us, 5.1 TB/s, with two-byte stores of values 22.6; of 3 x 1024 rows of 16 and 2 into
-// an int8 cache, 30 MB: 9.7 us; gather of 24400 rows of 2 kv heads, 50 MB: 10.4 us, of 18000 int8 rows, 28 MB: 8.1 us.)
+// (Append of 9500 rows of 8 query and 2 kv heads, 58 MB: 11.8 us, 4.9 TB/s, with two-byte stores of values 22.6; of 3 x 1024 rows of 16 and 2 into
+// an int8 cache, 30 MB: 10.1 us; gather of 24400 rows of 2 kv heads, 50 MB: 9.7 us, of 18000 int8 rows, 28 MB: 8.3 us.)
 #include "rows.h"
 
 namespace psv {

@@ -6,8 +6,9 @@
 // common rounding of the exponents, at most a quarter of a unit (below).
 //
 // A piece is read once, into registers, all loads at once, and everything else -- the maximum, the sums, the alternatives -- is made from
-// there.  Large calls in 32 bits are bound by memory (1024 rows of 128256, 525 MB: 92 us, 5.7 TB/s), in 16 bits by instructions, 11.4 a column of
-// which the exponential takes the time of four (2048 rows, the same bytes: 101 us, the vector units busy 92 % of it).  Small ones are bound by
+// there.  Large calls in 32 bits are bound by memory (1024 rows of 128256, 525 MB: 92 us, 5.7 TB/s), in 16 bits by instructions, 11.3 a column of
+// which the exponential takes the time of four (2048 rows, the same bytes: 102 us, the vector units busy 89 % of it; both for 8 alternatives, without the
+// join, in a stream of calls).  Small ones are bound by
 // the chain load -> bound -> candidates -> ranks, 5 us, and the same in the join.
 //
 // Alternatives without sorting: the top-th largest of the lanes' maxima is a bound T that at least `top` logits reach, and of every lane
@@ -237,7 +238,8 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
     const bool bad = top_order >= kOrderInf;          // a NaN or +infinity
     const float M = of_order(top_order), ref = top_order == kOrderNone ? 0.f : M;
     // In units of log 2, t = x c - M c as one multiply-add: M c is rounded, which moves every t by the same `shift`, known exactly and taken out of
-    // the sums at their end.  (With the difference first a column costs an instruction more: 2048 rows of 128256 in bf16 108.8 us against 100.6.)
+    // the sums at their end.  (With the difference first a column costs an instruction more: this kernel, 2048 rows of 128256 in bf16 108.8 us
+    // against 100.6.)
     // Below 2^23 the rounding is at most 1/4, which scales the sums by 2^(1/4) at most and costs the second a quarter of the first's error.  From there
     // on -- a large scale, or a piece of nothing but far values -- it would leave the exponential's range: the difference first, of columns read again.
     const float c = g.to_log2;
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
         for (int i = 0; i < E / G; ++i) groups |= most[i] >= least ? 1u << i : 0u;
         auto id_of = [&](uint32_t i, uint32_t e) { return c0 + threadIdx.x * N + i * (G * kThreads) + e / N * (kThreads * N) + e % N; };
         // Taken from the registers, a group costs a selection a word and group: large pieces, which are bound by their instructions, read it
-        // again instead (2048 rows of 32000 in bf16, 20 alternatives: 38.0 us against 40.2); small ones would wait for the trip.
+        // again instead (this kernel, 2048 rows of 32000 in bf16, 20 alternatives: 38.0 us against 40.2); small ones would wait for the trip.
         auto group = [&](uint32_t i) {
             if constexpr (E < 64) {
                 return x.group(i);
@@ -308,7 +310,7 @@ __global__ __launch_bounds__(kLogprobThreads, DT == PSV_F32 ? (E == 128 ? 2 : E 
                     for (int e = 0; e < G; ++e)
                         if (h.get(e) == least && id_of(i, e) > last) hits &= ~(1u << e);
                 uint32_t at = list_places(&sh.count, (uint32_t)__popc(hits));
-                // A step a hit, mostly one, not a test a column (61 rows of 32003 for 20: 7.0 us against 7.4; 2048 of 128256: 114 against 117)
+                // A step a hit, mostly one, not a test a column (for 20, this kernel, 61 rows of 32003: 7.0 us against 7.4; with the join, 2048 of 128256: 114 against 117)
                 for (; hits && at < kList; hits &= hits - 1) {
                     const uint32_t e = __builtin_ctz(hits);
                     sh.list[at++] = list_entry(order_of(h.pick(e)), id_of(i, e));

@@ -1,9 +1,9 @@
 // Rotary positions of rows (psv_rotate): every channel pair (a, b) of the first n channels of a head becomes
 // (a c - b s, b c + a s), c and s the cosine and sine of position times frequency.
 //
-// Bound by memory: a row is read and written once, 16 bytes a lane (16384 rows of 16 heads in 32 bits, 268 MB: 49.9 us, 5.4 TB/s).  The angles
+// Bound by memory: a row is read and written once, 16 bytes a lane (16384 rows of 16 heads in 32 bits, 268 MB: 50.4 us, 5.3 TB/s).  The angles
 // are formed and reduced in 64 bits, once for each row and pair, by the workgroup that has the row, and lie in LDS for all of its heads; rows of
-// one head pay for them (65536 rows of one head, 34 MB: 17.4 us).
+// one head pay for them (65536 rows of one head in 16 bits, 34 MB: 18.3 us).
 #include "rows.h"
 
 namespace psv {
@@ -94,7 +94,9 @@ __global__ __launch_bounds__(kRotateThreads) void k_rotate(RotateArgs g)
     }
 }
 
-// Rows of any alignment and heads of any size: one pair, or one channel, a lane and step.
+// Rows of any alignment and heads of any size: one pair, or one channel, a lane and step.  Bound by its instructions and small accesses: 16384 rows of
+// 16 heads one element off 16 bytes 64.4 us in 32 bits and 46.8 in 16 (2.9 TB/s); in 16 bits 40 of 80 channels rotated in halves 41.5 (2.0 TB/s; in neighbours,
+// by the kernel above, 16.3), 24 of 96 60.5 (1.7).
 template <uint32_t DT, bool HALF>
 __global__ __launch_bounds__(kRotateThreads) void k_rotate_any(RotateArgs g)
 {

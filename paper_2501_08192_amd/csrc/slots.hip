@@ -3,7 +3,7 @@
 // Two prefix sums over the requests (rows and blocks), which also say who is refused, then 16 bytes a row.  The sums are a few
 // thousand additions: every workgroup makes them for itself, so that one launch does all and no workgroup waits for another; its
 // rows are then spread over the lanes, four neighbours each, their request found by bisection of the row starts in LDS.  Bound by the launch
-// and the chain lengths -> sums -> row starts -> block -> slot: 64 requests of one token 3.2 us, 509 of 400 tokens (3.3 MB)
+// and the chain lengths -> sums -> row starts -> block -> slot: 64 requests of one token 3.4 us, 509 of 400 tokens (3.3 MB)
 // 7.0.
 //
 // Why both sums can be made at once, though a request whose rows do not fit takes no blocks: the rows before it only grow, so that one
