@@ -57,3 +57,21 @@ def test_append_of_the_most_rows(rows, nkv, layout):
     rest = np.setdiff1d(np.arange(blocks * 16), places.cpu())
     for (a, _), (b, _) in zip(pools.rows(pools.gpu, rest), pools.rows(pools.before, rest)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("widths,records", [([40] * 256, 1), ([9] * 128 + [33] * 128, 1), ([700] * 2, 128), ([3000] * 16, 16)])
+def test_log_probabilities_joined_from_the_most_records(widths, records):
+    """256 records of 32 alternatives: ordinary rows, rows of equal logits, steps of equal ones, rows that one record has all the largest of."""
+    from test_gpu_logprobs import check, given, logits
+    v = sum(widths)
+    x = logits(8, v, "bf16", seed=14)
+    x[1] = 0.0
+    x[2] = (torch.arange(v) // 50 % 7).bfloat16().cuda()
+    x[3] = (torch.arange(v) % 31 == 0).bfloat16().cuda()
+    x[4, v - 40:] = 20.0
+    x[5] = -float("inf")
+    x[5, ::max(1, v // 20)] = 1.0
+    x[6] = torch.arange(v, 0, -1).bfloat16().cuda() / 64
+    x[7, widths[0]:] = -1e10
+    check(x, given(8, v, 2, 14), top=32, shards=widths, records=records)
+    check(x, given(8, v, 2, 14), top=3, shards=widths, records=records)
